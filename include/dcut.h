@@ -20,6 +20,14 @@
  *   dcut_select_rs       shifted scores with a causal budget choice
  *   dcut_accept_rs       RS acceptance with residual sampling
  *
+ * For engines that keep the cache in pages, the attention step of a layer on
+ * such a cache:
+ *
+ *   dcut_paged_append        rotation of the new queries and keys, append to the pages
+ *   dcut_paged_attn          ragged causal attention over the pages
+ *   dcut_paged_attn_shared   the same, a prefix that requests share read once
+ *   dcut_paged_attn_sparse   the same over the pages a score selects per query
+ *
  * Conventions shared by every call
  *   - All pointers marked "dev" are device pointers on the current HIP device;
  *     "host" pointers are read during the call only.  The caller owns every
@@ -42,7 +50,8 @@
  *     are launched for the maximum B(D+1) rows and read K* = cu[B] on the device.
  *   - Matrices follow PyTorch nn.Linear layout [out][in], row-major; bf16 values
  *     are raw bits (dcut_bf16), rounded to nearest-even by the producer.
- *   - Supported sizes: 1 <= B <= 4096, 0 <= D, D + 1 <= 64, B (D + 1) <= 8192.
+ *   - Supported sizes: 1 <= B <= 4096, 0 <= D, D + 1 <= 64, B (D + 1) <= 8192
+ *     (the dcut_paged_* calls: see there).
  */
 #ifndef DCUT_H
 #define DCUT_H
@@ -70,7 +79,9 @@ enum {
 enum {
   DCUT_DERR_CONF = 1,      /* a confidence is NaN, has its sign bit set, or exceeds 1 */
   DCUT_DERR_TOKEN = 2,     /* a token id outside [0, vocab)                           */
-  DCUT_DERR_CAPACITY = 4   /* ctx_len < 0 or ctx_len + D + 1 > cap for some request   */
+  DCUT_DERR_CAPACITY = 4,  /* ctx_len < 0 or ctx_len + D + 1 > cap for some request   */
+  DCUT_DERR_PAGE = 8,      /* a page number outside [0, n_pages)                      */
+  DCUT_DERR_GROUP = 16     /* a shared prefix longer than a member's context          */
 };
 
 enum { DCUT_MAX_BLOCK = 64, DCUT_MAX_BATCH = 4096, DCUT_MAX_ROWS = 8192, DCUT_MAX_CANDIDATES = 64 };
@@ -367,6 +378,146 @@ int dcut_accept_rs(int B, int D, int V, float temperature, uint64_t seed, const 
                    int32_t *ctx_len_inout, void *ws, size_t ws_bytes, int32_t *dev_err,
                    hipStream_t stream);
 
+/*
+ * The paged key/value cache.
+ *
+ * Keys and values lie in pages of `page` keys: k and v are [n_pages][n_kv][page]
+ * [head_dim] bf16, and key j of request i (keys stored after the rotation) is slot
+ * j % page of page table[i * table_ld + j / page].  Several requests may list the
+ * same page.  Table entries past a request's last page are never read.  Slots past
+ * a request's last key may hold anything, infinities and NaN too.
+ * kmin, kmax (NULL unless used) are the channel bounds [n_pages][n_kv][head_dim]
+ * bf16 of every full page's keys: dcut_paged_append keeps them, dcut_paged_attn_sparse
+ * reads them.
+ *
+ * dcut_paged_cfg bounds a launch from the host (contexts and kept rows stay on the
+ * device): max_ctx the keys a request may see, its new rows included; max_block the
+ * new rows of one request; max_rows those of the batch, cu[B].  One captured graph
+ * serves every batch within the bounds.
+ * Supported: head_dim 64 or 128; page 16, 32, 64, 128 or 256; n_q % n_kv == 0,
+ * n_q / n_kv <= 64, n_q <= 1024; max_block <= max_ctx <= 2^24; max_rows <= 131072;
+ * 1 <= B <= 4096.  Pools of any size (addresses are 64 bits).
+ */
+typedef struct {
+  int n_q, n_kv, head_dim;
+  int page;
+  int max_ctx, max_block, max_rows;
+} dcut_paged_cfg;
+
+typedef struct {
+  dcut_bf16 *k, *v;        /* dev, 16-byte aligned */
+  const int32_t *table;    /* dev [B][table_ld]    */
+  int n_pages, table_ld;
+  dcut_bf16 *kmin, *kmax;  /* dev, 16-byte aligned, or both NULL */
+} dcut_pages;
+
+enum { DCUT_BF16 = 0, DCUT_F32 = 1 };     /* element types of dcut_paged_append's input */
+enum { DCUT_PAGED_MAX_SEL = 4096 };       /* pages dcut_paged_attn_sparse may read a query */
+
+/*
+ * dcut_paged_append -- rotate the new rows' queries and keys, append keys and values.
+ *
+ * For row t < cu[B] with p = packed_pos[t], i = packed_req[t]: q and k are rotated
+ * as in dcut_verify_layer (pairs j, j + head_dim/2; angle p * rope_theta^(-2j/head_dim),
+ * formed in 64 bits); q goes to q_out[t], k and v to request i's key p.  With
+ * pages->kmin, every page whose last slot is written has its channel bounds taken
+ * over all of its keys as stored (a NaN key is left out).
+ * The keys of one call are distinct (requests append to pages of their own); a key
+ * written again replaces the old one, as after rejected drafts.
+ *
+ *   cu, packed_pos, packed_req   dev, from dcut_select, or the caller's own for prompts:
+ *           rows packed request by request, positions ascending by one within a request
+ *   type    DCUT_BF16 or DCUT_F32: elements of q, k and v
+ *   q, k, v dev [max_rows][heads * head_dim], row strides ldq, ldk, ldv in elements
+ *           (views of one fused projection); 16-byte aligned rows.  q and q_out may
+ *           both be NULL (append only)
+ *   q_out   dev [max_rows][n_q][head_dim] bf16 out (must not overlap the inputs)
+ *   dev_err DCUT_DERR_CAPACITY for a row whose request is outside [0, B) or whose
+ *           position lies outside the table or max_ctx, DCUT_DERR_PAGE for a bad page:
+ *           the row is not appended
+ * Rows from cu[B] on are neither read nor written.
+ * Returns DCUT_OK, DCUT_EINVAL, DCUT_EUNSUPPORTED, DCUT_EHIP.
+ */
+int dcut_paged_append(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B, const int32_t *cu,
+                      const int32_t *packed_pos, const int32_t *packed_req, int type, const void *q,
+                      int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, float rope_theta,
+                      dcut_bf16 *q_out, int32_t *dev_err, hipStream_t stream);
+
+/*
+ * dcut_paged_attn -- ragged causal attention of the new rows over the pages.
+ *
+ * Row t = cu[i] + r of request i (its L_i = ctx_len[i] earlier keys and the new rows'
+ * keys are in the cache): head h attends to keys 0 .. L_i + r of kv head
+ * h / (n_q / n_kv), scale 1/sqrt(head_dim).  One new row a request decodes, a kept
+ * block of drafts verifies, any number is a (piece of a) prompt; requests without
+ * rows are skipped.  A key that a row does not see never reaches it, whatever it holds.
+ * A row whose scores are all minus infinity gives 0 and a log sum of minus infinity.
+ * A row's result depends on its own request and the launch bounds only: bitwise
+ * the same whatever other rows and requests hold.
+ *
+ *   q       dev [max_rows][n_q][head_dim] bf16, row stride ldq elements, a multiple of 8
+ *   cu      dev [B+1]; ctx_len dev [B]
+ *   out     dev [max_rows][n_q][head_dim] bf16 out, contiguous (may not overlap q)
+ *   lse     dev [max_rows][n_q] float32 out (nullable): ln sum exp of the row's scores
+ *   ws      dev scratch of dcut_paged_workspace_bytes(0, cfg, B, 0) bytes, 256-byte
+ *           aligned; calls that may overlap need scratch of their own
+ *   dev_err DCUT_DERR_CAPACITY (rows or context outside the bounds or the table; the
+ *           request's rows are unspecified), DCUT_DERR_PAGE
+ * Rows from cu[B] on are neither read nor written.
+ * Returns DCUT_OK, DCUT_EINVAL, DCUT_EUNSUPPORTED, DCUT_EWORKSPACE, DCUT_EHIP.
+ */
+int dcut_paged_attn(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B, const dcut_bf16 *q,
+                    int64_t ldq, const int32_t *cu, const int32_t *ctx_len, dcut_bf16 *out, float *lse,
+                    int32_t *dev_err, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * dcut_paged_attn_shared -- dcut_paged_attn for requests that share prefixes.
+ *
+ * Requests group_cu[g] .. group_cu[g+1]-1 of group g hold the same first prefix_len[g]
+ * keys (answers to one prompt, drafts under one system prompt): these are read through
+ * the first member's table, once for all of the group's rows, and each request's other
+ * keys through its own.  The result is dcut_paged_attn's up to the rounding of its sums
+ * and depends on the group's rows only through which of them exist.  prefix_len need not
+ * be a multiple of the page; 0 shares nothing, as do requests outside every group.
+ *
+ *   n_groups  1 .. B;  group_cu dev [n_groups+1] non-decreasing;  prefix_len dev [n_groups]
+ *   dev_err   also DCUT_DERR_GROUP where a prefix exceeds a member's ctx_len
+ *   ws        dcut_paged_workspace_bytes(1, cfg, B, 0)
+ *   other arguments as for dcut_paged_attn
+ */
+int dcut_paged_attn_shared(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B, const dcut_bf16 *q,
+                           int64_t ldq, const int32_t *cu, const int32_t *ctx_len, int n_groups,
+                           const int32_t *group_cu, const int32_t *prefix_len, dcut_bf16 *out, float *lse,
+                           int32_t *dev_err, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * dcut_paged_attn_sparse -- dcut_paged_attn over n_sel pages a query and kv head.
+ *
+ * Row t at position p = L_i + r with kv head g sees pages 0 .. p / page.  Pages
+ * j < n_sink and the last n_local are always read; the others are ranked by
+ *   sum_d max(q, 0)_d kmax[j]_d + min(q, 0)_d kmin[j]_d
+ * with max(q, 0) and min(q, 0) summed over the group's query heads, an upper bound of
+ * the group's summed scores with any key of page j, formed in 64 bits (NaN ranks last),
+ * ties to the lower page; n_sel pages are read in all, or every page if there are no
+ * more.  Attention as dcut_paged_attn over the visible keys of these pages.
+ *
+ *   n_sel    1 .. 4096;  n_sink >= 0;  n_local >= 1;  n_sink + n_local <= n_sel
+ *   blocks   dev [max_rows][n_kv][n_sel] int32 out (nullable): the table columns of the
+ *            pages read, ascending, then -1
+ *   pages    with kmin and kmax of every full page
+ *   ws       dcut_paged_workspace_bytes(2, cfg, B, n_sel)
+ *   other arguments as for dcut_paged_attn
+ */
+int dcut_paged_attn_sparse(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B, const dcut_bf16 *q,
+                           int64_t ldq, const int32_t *cu, const int32_t *ctx_len, int n_sel, int n_sink,
+                           int n_local, int32_t *blocks, dcut_bf16 *out, float *lse, int32_t *dev_err,
+                           void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Scratch bytes of the paged attention calls: which = 0 dcut_paged_attn, 1 its shared
+ * form, 2 its sparse form (which reads n_sel).  0 when none is needed (ws may then be
+ * NULL), (size_t)-1 for a configuration the calls refuse. */
+size_t dcut_paged_workspace_bytes(int which, const dcut_paged_cfg *cfg, int B, int n_sel);
+
 /* Scratch bytes for call `which` (0 select and select_rs, 1 verify_layer,
  * 2 lm_head_argmax and lm_head_sample, 3 accept, 4 accept_rs, which reads
  * cfg->vocab); cfg may be NULL for 0 and 3.  Returns 0 when none is needed and
@@ -407,7 +558,9 @@ enum {
   DCUT_KERNEL_ARGMAX_FINAL, DCUT_KERNEL_ACCEPT, DCUT_KERNEL_RS_DECIDE, DCUT_KERNEL_RS_RESIDUAL,
   DCUT_KERNEL_RS_FINISH,
   DCUT_KERNEL_ATTN_PLAN /* no kernel of its own: the attention work order is built by an extra
-                           workgroup of the layer's first norm kernel */
+                           workgroup of the layer's first norm kernel */,
+  DCUT_KERNEL_PAGED_APPEND, DCUT_KERNEL_PAGED_BOUNDS, DCUT_KERNEL_PAGED_ATTN,
+  DCUT_KERNEL_PAGED_PREFIX, DCUT_KERNEL_PAGED_MERGE, DCUT_KERNEL_PAGE_SCORE, DCUT_KERNEL_PAGE_SELECT
 };
 int dcut_profile_arm(int kernel, hipEvent_t start, hipEvent_t stop);
 

@@ -1,6 +1,7 @@
 // Host-side helpers of the C ABI: status strings, workspace sizes, budgets from
 // ratios (Eq. dcut-budget), nearest captured batch (App. C), profiling hook.
 #include "dcut_internal.h"
+#include "paged.h"
 
 namespace dcut {
 size_t layer_ws_bytes(const dcut_layer_cfg *c, int B, int D);
@@ -42,6 +43,16 @@ extern "C" size_t dcut_workspace_bytes(int which, const dcut_layer_cfg *cfg, int
   return (size_t)-1;
 }
 
+extern "C" size_t dcut_paged_workspace_bytes(int which, const dcut_paged_cfg *cfg, int B, int n_sel) {
+  if (paged_cfg_check(cfg, B) != DCUT_OK) return (size_t)-1;
+  switch (which) {
+    case 0: return paged_attn_ws_bytes(cfg, B, false);
+    case 1: return paged_attn_ws_bytes(cfg, B, true);
+    case 2: return n_sel < 1 || n_sel > DCUT_PAGED_MAX_SEL ? (size_t)-1 : paged_sparse_ws_bytes(cfg, n_sel);
+  }
+  return (size_t)-1;
+}
+
 extern "C" int dcut_budgets_from_ratios(int B, int D, int R, const int32_t *num, const int32_t *den,
                                         int32_t *out) {
   if (!batch_ok(B, D) || R < 1 || R > DCUT_MAX_CANDIDATES || !num || !den || !out) return DCUT_EINVAL;
@@ -68,7 +79,7 @@ extern "C" int dcut_nearest_batch(int B, int n, const int32_t *captured) {
 }
 
 extern "C" int dcut_profile_arm(int kernel, hipEvent_t start, hipEvent_t stop) {
-  if (kernel < DCUT_KERNEL_NONE || kernel > DCUT_KERNEL_ATTN_PLAN) return DCUT_EINVAL;
+  if (kernel < DCUT_KERNEL_NONE || kernel > DCUT_KERNEL_PAGE_SELECT) return DCUT_EINVAL;
   if (kernel != DCUT_KERNEL_NONE && (!start || !stop)) return DCUT_EINVAL;
   ProfileHook &h = profile_hook();
   h.kernel = kernel;

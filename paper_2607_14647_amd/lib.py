@@ -17,16 +17,20 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libdcut.so")
 
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, -1, -2, -3, -4
-DERR_CONF, DERR_TOKEN, DERR_CAPACITY = 1, 2, 4
+DERR_CONF, DERR_TOKEN, DERR_CAPACITY, DERR_PAGE, DERR_GROUP = 1, 2, 4, 8, 16
 KERNELS = dict(NONE=0, SELECT=1, PACK=2, NORM=3, GEMM_QKV=4, ATTN=5, ATTN_COMBINE=6, GEMM_O=7,
                GEMM_GATE_UP=8, GEMM_DOWN=9, MOE=10, LM_HEAD=11, ARGMAX_FINAL=12, ACCEPT=13,
-               RS_DECIDE=14, RS_RESIDUAL=15, RS_FINISH=16, ATTN_PLAN=17)
+               RS_DECIDE=14, RS_RESIDUAL=15, RS_FINISH=16, ATTN_PLAN=17, PAGED_APPEND=18, PAGED_BOUNDS=19, PAGED_ATTN=20, PAGED_PREFIX=21,
+               PAGED_MERGE=22, PAGE_SCORE=23, PAGE_SELECT=24)
 RS_SCAN, RS_FIXED, RS_HISTORY = 0, 1, 2
+BF16, F32 = 0, 1
+PAGED_CALLS = dict(attn=0, shared=1, sparse=2)
 
 EXPORTS = ["dcut_select", "dcut_verify_layer", "dcut_lm_head_argmax", "dcut_lm_head_argmax_static",
            "dcut_lm_head_static_scratch_bytes", "dcut_accept", "dcut_lm_head_sample", "dcut_select_rs",
            "dcut_accept_rs", "dcut_workspace_bytes", "dcut_strerror", "dcut_budgets_from_ratios",
-           "dcut_nearest_batch", "dcut_profile_arm", "dcut_stream_probe"]
+           "dcut_nearest_batch", "dcut_profile_arm", "dcut_stream_probe", "dcut_paged_append", "dcut_paged_attn",
+           "dcut_paged_attn_shared", "dcut_paged_attn_sparse", "dcut_paged_workspace_bytes"]
 
 
 class DcutError(RuntimeError):
@@ -52,6 +56,15 @@ class LayerW(C.Structure):
 
 class KV(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("base", C.c_void_p), ("cap", C.c_void_p)]
+
+
+class PagedCfg(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_q", "n_kv", "head_dim", "page", "max_ctx", "max_block", "max_rows")]
+
+
+class Pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("n_pages", C.c_int), ("table_ld", C.c_int),
+                ("kmin", C.c_void_p), ("kmax", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -80,7 +93,14 @@ def _load() -> C.CDLL:
     lib.dcut_nearest_batch.argtypes = [i32, i32, vp]
     lib.dcut_profile_arm.argtypes = [i32, vp, vp]
     lib.dcut_stream_probe.argtypes = [vp, sz, i32, vp]
-    for f in ["dcut_select", "dcut_verify_layer", "dcut_lm_head_argmax", "dcut_lm_head_argmax_static",
+    i64, cfgp, pgp = C.c_int64, C.POINTER(PagedCfg), C.POINTER(Pages)
+    lib.dcut_paged_append.argtypes = [cfgp, pgp, i32, vp, vp, vp, i32, vp, i64, vp, i64, vp, i64, C.c_float, vp, vp, vp]
+    lib.dcut_paged_attn.argtypes = [cfgp, pgp, i32, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dcut_paged_attn_shared.argtypes = [cfgp, pgp, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dcut_paged_attn_sparse.argtypes = [cfgp, pgp, i32, vp, i64, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.dcut_paged_workspace_bytes.argtypes = [i32, cfgp, i32, i32]
+    lib.dcut_paged_workspace_bytes.restype = sz
+    for f in ["dcut_paged_append", "dcut_paged_attn", "dcut_paged_attn_shared", "dcut_paged_attn_sparse", "dcut_select", "dcut_verify_layer", "dcut_lm_head_argmax", "dcut_lm_head_argmax_static",
               "dcut_lm_head_sample", "dcut_accept",
               "dcut_select_rs", "dcut_accept_rs", "dcut_budgets_from_ratios", "dcut_nearest_batch",
               "dcut_profile_arm"]:
@@ -265,6 +285,70 @@ def accept_rs(B: int, D: int, V: int, temperature: float, seed: int, draft: torc
                              _p(accept_len), _p(next_tok), _p(total), _p(ctx_len_inout), _p(ws),
                              ws.numel() * ws.element_size(), _p(dev_err), _stream(stream))
     _check(st, "dcut_accept_rs")
+
+
+# ------------------------------------------------------------------ the paged cache
+
+def paged_cfg(n_q: int, n_kv: int, head_dim: int, page: int, max_ctx: int, max_block: int, max_rows: int) -> PagedCfg:
+    return PagedCfg(int(n_q), int(n_kv), int(head_dim), int(page), int(max_ctx), int(max_block), int(max_rows))
+
+
+def pages_desc(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kmin: Optional[torch.Tensor] = None,
+               kmax: Optional[torch.Tensor] = None) -> Pages:
+    """Descriptor of a paged cache: k, v [n_pages][n_kv][page][head_dim], table [B][columns] int32 (its rows may be
+    strided), channel bounds kmin, kmax [n_pages][n_kv][head_dim] or None.  The descriptor keeps the tensors alive."""
+    p = lambda t: t.data_ptr() if t is not None else None
+    desc = Pages(p(k), p(v), p(table), k.shape[0], table.stride(0), p(kmin), p(kmax))
+    desc.tensors = (k, v, table, kmin, kmax)
+    return desc
+
+
+def paged_workspace_bytes(call: str, cfg: PagedCfg, B: int, n_sel: int = 0) -> int:
+    """Scratch bytes of paged_attn ("attn"), paged_attn_shared ("shared") or paged_attn_sparse ("sparse")."""
+    n = int(_lib.dcut_paged_workspace_bytes(PAGED_CALLS[call], C.byref(cfg), B, int(n_sel)))
+    if n == 2 ** (8 * C.sizeof(C.c_size_t)) - 1:
+        raise DcutError(EINVAL, "dcut_paged_workspace_bytes")
+    return n
+
+
+def paged_append(cfg: PagedCfg, pages: Pages, B: int, cu: torch.Tensor, packed_pos: torch.Tensor,
+                 packed_req: torch.Tensor, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                 q_out: Optional[torch.Tensor], theta: float, dev_err: Optional[torch.Tensor] = None,
+                 stream=None) -> None:
+    """q, k, v: [rows][...] of float32 or bf16 (also as raw 16-bit integers), rows of any stride."""
+    st = _lib.dcut_paged_append(C.byref(cfg), C.byref(pages), B, _p(cu), _p(packed_pos), _p(packed_req),
+                                F32 if k.dtype == torch.float32 else BF16, _p(q), q.stride(0) if q is not None else 0,
+                                _p(k), k.stride(0), _p(v), v.stride(0), float(theta), _p(q_out), _p(dev_err),
+                                _stream(stream))
+    _check(st, "dcut_paged_append")
+
+
+def paged_attn(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
+               out: torch.Tensor, ws: Optional[torch.Tensor], lse: Optional[torch.Tensor] = None,
+               dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
+    st = _lib.dcut_paged_attn(C.byref(cfg), C.byref(pages), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), _p(out), _p(lse),
+                              _p(dev_err), _p(ws), ws.numel() * ws.element_size() if ws is not None else 0,
+                              _stream(stream))
+    _check(st, "dcut_paged_attn")
+
+
+def paged_attn_shared(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
+                      out: torch.Tensor, ws: torch.Tensor, group_cu: torch.Tensor, prefix_len: torch.Tensor,
+                      lse: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
+    st = _lib.dcut_paged_attn_shared(C.byref(cfg), C.byref(pages), B, _p(q), q.stride(0), _p(cu), _p(ctx_len),
+                                     prefix_len.numel(), _p(group_cu), _p(prefix_len), _p(out), _p(lse), _p(dev_err),
+                                     _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "dcut_paged_attn_shared")
+
+
+def paged_attn_sparse(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
+                      out: torch.Tensor, ws: torch.Tensor, n_sel: int, n_sink: int, n_local: int,
+                      blocks: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                      dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
+    st = _lib.dcut_paged_attn_sparse(C.byref(cfg), C.byref(pages), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), int(n_sel),
+                                     int(n_sink), int(n_local), _p(blocks), _p(out), _p(lse), _p(dev_err), _p(ws),
+                                     ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "dcut_paged_attn_sparse")
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:

@@ -1,0 +1,132 @@
+"""The paged cache's entry points without a GPU: refusals before any launch, scratch sizes; its oracle's closed forms."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import paged as op
+from paper_2607_14647_amd import lib as L
+
+FAKE = C.c_void_p(0x1000)            # never dereferenced: validation fails first
+GOOD = dict(n_q=8, n_kv=2, head_dim=128, page=16, max_ctx=1000, max_block=4, max_rows=16)
+
+
+def _cfg(**kw):
+    return L.PagedCfg(*[{**GOOD, **kw}[n] for n, _ in L.PagedCfg._fields_])
+
+
+def _pages(**kw):
+    d = dict(k=0x1000, v=0x1000, table=0x1000, n_pages=4, table_ld=4, kmin=0x1000, kmax=0x1000)
+    d.update(kw)
+    return L.Pages(*[d[n] for n, _ in L.Pages._fields_])
+
+
+def _attn(cfg, pages=None, B=4, q=FAKE, ldq=1024, cu=FAKE, ctx=FAKE, out=FAKE, ws=None, wsb=0):
+    pages = _pages() if pages is None else pages
+    return L.lib().dcut_paged_attn(C.byref(cfg), C.byref(pages), B, q, ldq, cu, ctx, out, None, None, ws, wsb, None)
+
+
+def _shared(cfg, n_groups=1, gcu=FAKE, pre=FAKE, ws=None, wsb=0, B=4):
+    return L.lib().dcut_paged_attn_shared(C.byref(cfg), C.byref(_pages()), B, FAKE, 1024, FAKE, FAKE, n_groups, gcu, pre,
+                                          FAKE, None, None, ws, wsb, None)
+
+
+def _sparse(cfg, n_sel=8, n_sink=1, n_local=1, pages=None, ws=None, wsb=0):
+    pages = _pages() if pages is None else pages
+    return L.lib().dcut_paged_attn_sparse(C.byref(cfg), C.byref(pages), 4, FAKE, 1024, FAKE, FAKE, n_sel, n_sink, n_local,
+                                          None, FAKE, None, None, ws, wsb, None)
+
+
+def _append(cfg, pages=None, typ=L.BF16, q=FAKE, ldq=1024, k=FAKE, ldk=256, v=FAKE, ldv=256, theta=1e4, q_out=FAKE, pos=FAKE):
+    pages = _pages() if pages is None else pages
+    return L.lib().dcut_paged_append(C.byref(cfg), C.byref(pages), 4, FAKE, pos, FAKE, typ, q, ldq, k, ldk, v, ldv, theta,
+                                     q_out, None, None)
+
+
+BAD_CFG = [(dict(n_q=0), L.EINVAL), (dict(n_q=7), L.EINVAL), (dict(n_kv=0), L.EINVAL), (dict(head_dim=0), L.EINVAL),
+           (dict(page=0), L.EINVAL), (dict(max_ctx=0), L.EINVAL), (dict(max_block=0), L.EINVAL), (dict(max_rows=0), L.EINVAL),
+           (dict(max_block=1001), L.EINVAL), (dict(head_dim=96), L.EUNSUPPORTED), (dict(page=24), L.EUNSUPPORTED),
+           (dict(page=8), L.EUNSUPPORTED), (dict(page=512), L.EUNSUPPORTED), (dict(n_q=130, n_kv=2), L.EUNSUPPORTED),
+           (dict(max_rows=(1 << 17) + 1), L.EUNSUPPORTED), (dict(max_ctx=(1 << 24) + 1), L.EUNSUPPORTED)]
+
+
+@pytest.mark.parametrize("kw,want", BAD_CFG)
+def test_configurations_are_refused(kw, want):
+    cfg = _cfg(**kw)
+    ld = 1 << 16                       # wide enough for every head count here
+    assert _attn(cfg, ldq=ld) == want
+    assert L.lib().dcut_paged_attn_shared(C.byref(cfg), C.byref(_pages()), 4, FAKE, ld, FAKE, FAKE, 1, FAKE, FAKE, FAKE, None,
+                                          None, None, 0, None) == want
+    assert L.lib().dcut_paged_attn_sparse(C.byref(cfg), C.byref(_pages()), 4, FAKE, ld, FAKE, FAKE, 8, 1, 1, None, FAKE, None,
+                                          None, None, 0, None) == want
+    assert _append(cfg, ldq=ld, ldk=ld, ldv=ld) == want
+    with pytest.raises(L.DcutError):
+        L.paged_workspace_bytes("attn", cfg, 4)
+
+
+def test_arguments_are_refused():
+    c = _cfg()
+    assert _attn(c, B=0) == L.EINVAL and _attn(c, B=4097) == L.EINVAL
+    assert _attn(c, q=None) == L.EINVAL and _attn(c, cu=None) == L.EINVAL and _attn(c, ctx=None) == L.EINVAL
+    assert _attn(c, out=None) == L.EINVAL
+    assert _attn(c, q=C.c_void_p(0x1008)) == L.EINVAL and _attn(c, out=C.c_void_p(0x1008)) == L.EINVAL
+    assert _attn(c, ldq=1023) == L.EINVAL and _attn(c, ldq=1028) == L.EINVAL
+    for bad in (dict(k=None), dict(v=None), dict(table=None), dict(n_pages=0), dict(table_ld=0), dict(k=0x1008)):
+        assert _attn(c, pages=_pages(**bad)) == L.EINVAL
+        assert _append(c, pages=_pages(**bad)) == L.EINVAL
+        assert _sparse(c, pages=_pages(**bad)) == L.EINVAL
+    assert _shared(c, n_groups=0) == L.EINVAL and _shared(c, n_groups=5) == L.EINVAL
+    assert _shared(c, gcu=None) == L.EINVAL and _shared(c, pre=None) == L.EINVAL
+    assert _sparse(c, n_sel=0) == L.EINVAL and _sparse(c, n_local=0) == L.EINVAL and _sparse(c, n_sink=-1) == L.EINVAL
+    assert _sparse(c, n_sel=2, n_sink=1, n_local=2) == L.EINVAL
+    assert _sparse(c, n_sel=4097) == L.EUNSUPPORTED
+    assert _sparse(c, pages=_pages(kmin=None)) == L.EINVAL and _sparse(c, pages=_pages(kmax=0x1008)) == L.EINVAL
+    assert _append(c, typ=2) == L.EINVAL and _append(c, theta=0.0) == L.EINVAL and _append(c, theta=float("inf")) == L.EINVAL
+    assert _append(c, q=None) == L.EINVAL and _append(c, q_out=None) == L.EINVAL and _append(c, k=None) == L.EINVAL
+    assert _append(c, ldk=255) == L.EINVAL and _append(c, ldv=260) == L.EINVAL and _append(c, ldq=1020) == L.EINVAL
+    assert _append(c, pos=None) == L.EINVAL and _append(c, pages=_pages(kmin=None)) == L.EINVAL
+    assert _append(c, v=C.c_void_p(0x1002)) == L.EINVAL
+
+
+def test_workspaces_are_checked():
+    c = _cfg()
+    for call, which, run in (("attn", 0, _attn), ("shared", 1, _shared), ("sparse", 2, _sparse)):
+        n = L.paged_workspace_bytes(call, c, 4, 8)
+        assert n > 0 and n % 256 == 0
+        assert run(c) == L.EWORKSPACE
+        assert run(c, ws=FAKE, wsb=n - 1) == L.EWORKSPACE
+        assert run(c, ws=C.c_void_p(0x1010), wsb=n) == L.EWORKSPACE
+    assert L.lib().dcut_paged_workspace_bytes(3, C.byref(c), 4, 8) == 2 ** 64 - 1
+    assert L.lib().dcut_paged_workspace_bytes(2, C.byref(c), 4, 0) == 2 ** 64 - 1
+    # the partial sums do not grow without bound with the context: at most one per 2048 keys
+    # once a request has more than its share of pieces
+    big = _cfg(max_ctx=1 << 20, max_rows=512, n_q=32, n_kv=8)
+    assert L.paged_workspace_bytes("attn", big, 512) <= 512 * 32 * 512 * 132 * 4 + 4096
+
+
+def test_oracle_closed_forms():
+    """Equal keys give the mean of the values; a key far above the others gives its value; rotation keeps lengths and
+    turns position p by p times position 1's angle."""
+    rng = np.random.default_rng(3)
+    q, v = rng.standard_normal((4, 64)), rng.standard_normal((2, 7, 64))
+    out, lse, _, _ = op.attend(q, np.zeros((2, 7, 64)), v)
+    assert np.allclose(out, np.repeat(v.mean(1), 2, 0)) and np.allclose(lse, np.log(7))
+    k = np.zeros((2, 7, 64))
+    k[:, 3] = 0
+    k[0, 3], k[1, 3] = 1e4 * q[:2].sum(0), 1e4 * q[2:].sum(0)
+    out, _, _, _ = op.attend(q, k, v)
+    for h in range(4):
+        if (q[h] * (q[:2] if h < 2 else q[2:]).sum(0)).sum() > 1:
+            assert np.allclose(out[h], v[h // 2, 3])
+    x = rng.standard_normal((3, 2, 64))
+    r1, r5 = op.rotate(x, np.array([1, 1, 1]), 1e4), op.rotate(x, np.array([5, 5, 5]), 1e4)
+    assert np.allclose((r1 ** 2).sum(-1), (x ** 2).sum(-1))
+    for _ in range(4):
+        r1 = op.rotate(r1, np.array([1, 1, 1]), 1e4)
+    assert np.allclose(r1, r5)
+    # the score bounds the group's summed scores with every key of the page
+    kk = rng.standard_normal((5, 16, 64))
+    qs = rng.standard_normal((3, 64))
+    score = np.maximum(qs, 0).sum(0) @ kk.max(1).T + np.minimum(qs, 0).sum(0) @ kk.min(1).T
+    assert ((kk @ qs.sum(0)).max(1) <= score).all()
+    assert op.select_pages(qs, kk.min(1), kk.max(1), 3, 1, 1) == sorted({0, 4, 1 + int(np.argmax(score[1:4]))})
