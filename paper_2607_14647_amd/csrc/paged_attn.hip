@@ -16,26 +16,13 @@
 // Keys and values arrive through a ring of LDS stages (buffer loads with the LDS destination);
 // every wave load of 1 KB lies in one page, whose number is one scalar load, asked for a tile
 // ahead.  Keys outside the chunk read as zeros, whatever stale slots hold.
-#include "paged.h"
+#include "paged_item.h"
 
 namespace dcut {
 
 namespace {
 
-constexpr int KT = 32;     // keys per tile
-
-typedef short short4v __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(3))) const bf16x8 lds_frag;
-
-// Barrier of the LDS ring: each wave has waited (s_waitcnt vmcnt) for its own loads of the
-// stage it reads next, so only the hardware barrier is needed; a memory fence here would
-// drain every stage still in flight.
-__device__ __forceinline__ void ring_barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
+constexpr int KT = KEY_ALIGN;     // keys per tile
 
 // Transposing LDS reads of four column tiles x two key halves, the second half HALF bytes
 // after the first, issued and awaited in one statement.
@@ -54,146 +41,6 @@ __device__ __forceinline__ void lds_read_tr16_x8(short4v (&r)[8], uint32_t a0, u
       : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
       : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(HALF)
       : "memory");
-}
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void *base, int bytes) {
-  const uintptr_t b = (uintptr_t)base;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
-  return __builtin_amdgcn_make_buffer_rsrc((void *)(((uintptr_t)hi << 32) | lo), (short)0, bytes, 0x00020000);
-}
-
-enum Mode { OWN = 0, PREFIX = 1, LIST = 2 };
-
-// What a work item reads and computes; uniform over the workgroup.
-struct Item {
-  int g;               // kv head
-  int t0, rows, r0;    // first packed row of the unit, its (row, head) pairs, first of this tile
-  const int32_t *tab;  // page of keys j*page.. of the unit
-  int klo, kend;       // keys of the chunk; below klo and from kend on: none
-  int kstart;          // first key tile, a multiple of 32
-  int diag;            // packed row t0 + r sees keys up to diag + r
-  int nc, slot;        // partials of the rows, and which this one is
-  bool first;          // this item notes the rows' count of partials
-};
-
-// The unit a launch index names, where units are tiles of TM pairs of consecutive runs:
-// run i's tiles are numbered from floor(start_i G / TM) + i on, which no two runs share.
-template <int THREADS, typename Start>
-__device__ __forceinline__ int find_run(int n, int u, int *s_cnt, Start first_tile) {
-  int cnt = 0;
-  for (int j = threadIdx.x; j < n; j += THREADS) cnt += first_tile(j) <= u;
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) cnt += __shfl_xor(cnt, off, 64);
-  if ((threadIdx.x & 63) == 0) s_cnt[threadIdx.x >> 6] = cnt;
-  __syncthreads();
-  cnt = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) cnt += s_cnt[w];
-  __syncthreads();
-  return __builtin_amdgcn_readfirstlane(cnt) - 1;
-}
-
-// Keys of the group's prefix that request i reads through it (0: none), and its chunks.
-__device__ __forceinline__ int shared_prefix(const PagedArgs &a, int grp) {
-  const int lo = a.group_cu[grp], hi = a.group_cu[grp + 1], P = a.prefix_len[grp];
-  if (lo < 0 || hi > a.B || lo >= hi || P <= 0) return 0;
-  return P;
-}
-
-template <int MODE, int TM, int THREADS>
-__device__ __forceinline__ bool make_item(const PagedArgs &a, int idx, int units, int *s_cnt, Item &it) {
-  it.g = idx % a.n_kv;
-  const int rest = idx / a.n_kv;
-  const int u = rest % units;
-  const int c = rest / units;
-  if (MODE == LIST) {
-    const int t = u;
-    if (t >= a.cu[a.B] || t >= a.max_rows) return false;
-    const int n = a.list_keys[t * a.n_kv + it.g];
-    it.t0 = t; it.rows = a.G; it.r0 = 0;
-    it.tab = a.list + ((size_t)t * a.n_kv + it.g) * a.n_sel;
-    it.nc = split_count(a.split, n);
-    if (n <= 0 || c >= it.nc) return false;
-    const int ch = split_chunk(a.split, n);
-    it.kstart = it.klo = c * ch;
-    it.kend = min(n, it.klo + ch);
-    it.diag = n - 1;
-    it.slot = c;
-    it.first = c == 0 && it.g == 0;
-    return true;
-  }
-  if (MODE == PREFIX) {
-    auto first_tile = [&](int j) {
-      const int lo = min(max(a.group_cu[j], 0), a.B);
-      return (int)((long long)a.cu[lo] * a.G / TM) + j;
-    };
-    const int grp = find_run<THREADS>(a.n_groups, u, s_cnt, first_tile);
-    if (grp < 0) return false;
-    const int P = shared_prefix(a, grp);
-    if (P == 0) return false;
-    const int lo = a.group_cu[grp], hi = a.group_cu[grp + 1];
-    it.t0 = a.cu[lo];
-    const int d = a.cu[hi] - it.t0;
-    if (it.t0 < 0 || d <= 0 || it.t0 > a.max_rows - d) return false;
-    it.rows = d * a.G;
-    const long long r0 = ((long long)u - first_tile(grp)) * TM;
-    if (r0 < 0 || r0 >= it.rows) return false;
-    it.r0 = (int)r0;
-    if ((long long)P > (long long)a.table_ld << a.lpage || P > a.max_ctx) return false;
-    it.tab = a.table + (size_t)lo * a.table_ld;
-    const int ncp = split_count(a.psplit, P);
-    if (c >= ncp) return false;
-    const int ch = split_chunk(a.psplit, P);
-    it.kstart = it.klo = c * ch;
-    it.kend = min(P, it.klo + ch);
-    it.diag = 1 << 30;
-    it.nc = 2;
-    it.slot = c;
-    it.first = false;
-    return true;
-  }
-  int i = u;
-  long long r0 = 0;
-  if (a.G * a.max_block > TM) {
-    auto first_tile = [&](int j) { return (int)((long long)a.cu[j] * a.G / TM) + j; };
-    i = find_run<THREADS>(a.B, u, s_cnt, first_tile);
-    if (i < 0) return false;
-    r0 = ((long long)u - first_tile(i)) * TM;
-  }
-  ReqRows r;
-  if (!paged_request(a, i, c == 0 && it.g == 0 && threadIdx.x == 0, r)) return false;
-  it.t0 = r.t0;
-  it.rows = r.d * a.G;
-  if (r0 < 0 || r0 >= it.rows) return false;
-  it.r0 = (int)r0;
-  it.tab = a.table + (size_t)i * a.table_ld;
-  int P = 0, ncp = 0;
-  if (a.n_groups > 0) {
-    // the last group that starts at or before i, if it holds i
-    const int grp = find_run<THREADS>(a.n_groups, i, s_cnt, [&](int j) { return a.group_cu[j]; });
-    if (grp >= 0 && i < a.group_cu[grp + 1]) {
-      P = shared_prefix(a, grp);
-      if (P > r.L) {
-        if (c == 0 && it.g == 0 && threadIdx.x == 0 && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_GROUP);
-        P = 0;
-      } else if (P > 0) {
-        ncp = split_count(a.psplit, P);
-      }
-    }
-  }
-  const int nc = split_count(a.split, r.L - P);
-  if (c >= nc) return false;
-  const int ch = split_chunk(a.split, r.L - P);
-  const int last_row = (min(it.r0 + TM, it.rows) - 1) / a.G;
-  it.klo = P + c * ch;
-  it.kend = c == nc - 1 ? r.L + last_row + 1 : P + (c + 1) * ch;
-  it.kstart = it.klo & ~(KT - 1);
-  it.diag = r.L;
-  it.nc = ncp + nc;
-  it.slot = ncp + c;
-  it.first = c == 0 && it.g == 0;
-  return true;
 }
 
 // A wave owns RB blocks of 16 rows, 16 * NW rows apart.
@@ -386,10 +233,10 @@ k_paged_attn(PagedArgs a, int units) {
       // V^T fragment with the same keys comes from two transposing reads.
       bf16x8 pf;
       uint32_t *pw = (uint32_t *)&pf;
-      pw[0] = pack_bf2(s4[0][0], s4[0][1]);
-      pw[1] = pack_bf2(s4[0][2], s4[0][3]);
-      pw[2] = pack_bf2(s4[1][0], s4[1][1]);
-      pw[3] = pack_bf2(s4[1][2], s4[1][3]);
+      pw[0] = cvt_bf2(s4[0][0], s4[0][1]);
+      pw[1] = cvt_bf2(s4[0][2], s4[0][3]);
+      pw[2] = cvt_bf2(s4[1][0], s4[1][1]);
+      pw[3] = cvt_bf2(s4[1][2], s4[1][3]);
       static_assert(NT % 4 == 0 && KT == 32, "transposing reads come in groups of four columns, one 32-key step");
 #pragma unroll
       for (int n0 = 0; n0 < NT; n0 += 4) {
@@ -451,8 +298,8 @@ k_paged_attn(PagedArgs a, int units) {
       uint16_t *op = a.out + pair * HD;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        *(uint2 *)(op + 16 * n + 4 * grp4) = make_uint2(pack_bf2(o[rb][n][0] * inv, o[rb][n][1] * inv),
-                                                        pack_bf2(o[rb][n][2] * inv, o[rb][n][3] * inv));
+        *(uint2 *)(op + 16 * n + 4 * grp4) = make_uint2(cvt_bf2(o[rb][n][0] * inv, o[rb][n][1] * inv),
+                                                        cvt_bf2(o[rb][n][2] * inv, o[rb][n][3] * inv));
       if (a.lse && grp4 == 0) a.lse[pair] = 0.6931471805599453f * (m_run[rb] + __builtin_amdgcn_logf(l_run[rb]));
     } else {
       float *pp = a.part + (pair * a.MC + it.slot) * ATTN_PITCH(HD);
@@ -528,7 +375,7 @@ k_paged_merge(PagedArgs a) {
   const float inv = lsum > 0.0f ? 1.0f / lsum : lsum == 0.0f ? 0.0f : lsum;
   uint16_t *op = a.out + (size_t)pair * HD + lane * PER;
 #pragma unroll
-  for (int e = 0; e < PER; e += 2) *(uint32_t *)(op + e) = pack_bf2(acc[e] * inv, acc[e + 1] * inv);
+  for (int e = 0; e < PER; e += 2) *(uint32_t *)(op + e) = cvt_bf2(acc[e] * inv, acc[e + 1] * inv);
   if (a.lse && lane == 0) a.lse[pair] = 0.6931471805599453f * (mx + __builtin_amdgcn_logf(lsum));
 }
 
