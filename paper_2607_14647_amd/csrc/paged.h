@@ -84,10 +84,13 @@ __device__ __forceinline__ int uniform_load(const int32_t *p, int idx) {
 // Host side: argument checks and the split rule (paged_attn.hip).
 int paged_cfg_check(const dcut_paged_cfg *c, int B);
 int paged_pages_check(const dcut_paged_cfg *c, const dcut_pages *p);
-Split paged_split(long long units, bool capped);
+Split paged_split(long long units, int items, bool capped);
 int split_max(const Split &s, int max_keys);
 PagedArgs paged_args(const dcut_paged_cfg *c, const dcut_pages *p, int B, const dcut_bf16 *q, long long ldq,
                      const int32_t *cu, const int32_t *ctx_len, dcut_bf16 *out, float *lse, int32_t *dev_err);
+// Units of many rows (paged_tile.hip): rows of a tile, the launch.
+int paged_tile_rows();
+int paged_tile_launch(const PagedArgs &a, int head_dim, bool prefix, int units, int mc, hipStream_t s);
 int paged_list_attn_launch(const PagedArgs &a, int head_dim, hipStream_t s);
 size_t paged_attn_ws_bytes(const dcut_paged_cfg *c, int B, bool shared);
 size_t paged_sparse_ws_bytes(const dcut_paged_cfg *c, int n_sel);

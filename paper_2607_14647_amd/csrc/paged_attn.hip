@@ -22,7 +22,7 @@ namespace dcut {
 
 namespace {
 
-constexpr int KT = KEY_ALIGN;     // keys per tile
+constexpr int KT = 32;     // keys per tile
 
 // Transposing LDS reads of four column tiles x two key halves, the second half HALF bytes
 // after the first, issued and awaited in one statement.
@@ -62,7 +62,7 @@ k_paged_attn(PagedArgs a, int units) {
   __shared__ int s_cnt[NW];
 
   Item it;
-  if (!make_item<MODE, TM, NW * 64>(a, blockIdx.x, units, s_cnt, it)) return;
+  if (!make_item<MODE, TM, NW * 64, KT>(a, blockIdx.x, units, s_cnt, it)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, grp4 = lane >> 4;
@@ -390,22 +390,27 @@ int launch_items(const PagedArgs &a, int units, int mc, hipStream_t s) {
                 dim3((unsigned)grid), dim3(NW * 64), 0, s, a, units);
 }
 
-// Rows of a tile: 64 (a block of 16 a wave) where a unit has no more, else 128.
-int tile_rows(long long pairs) { return pairs <= 64 ? 64 : 128; }
-
-int own_units(const dcut_paged_cfg *c, int B) {
-  const int G = c->n_q / c->n_kv, TM = tile_rows((long long)G * c->max_block);
-  return (long long)G * c->max_block <= TM ? B : (int)tile_bound(c->max_rows, G, TM, B);
+// How the (row, query head) pairs of a unit are tiled: 64 (a block of 16 a wave) where a unit
+// has no more, 128, or the wide kernel's tiles.
+struct Tiling {
+  int rows;
+  bool wide;
+};
+Tiling tiling(long long pairs) {
+  if (pairs <= 64) return {64, false};
+  if (pairs <= 128) return {128, false};
+  return {paged_tile_rows(), true};
 }
 
 template <int HD, int MODE>
-int launch_mode(const PagedArgs &a, int units, int mc, int TM, hipStream_t s) {
-  if (TM == 64) return launch_items<HD, 4, 3, 1, MODE>(a, units, mc, s);
+int launch_mode(const PagedArgs &a, int units, int mc, int rows, hipStream_t s) {
+  if (rows == 64) return launch_items<HD, 4, 3, 1, MODE>(a, units, mc, s);
   return launch_items<HD, 4, 3, 2, MODE>(a, units, mc, s);
 }
 template <int MODE>
-int launch_hd(const PagedArgs &a, int hd, int units, int mc, int TM, hipStream_t s) {
-  return hd == 128 ? launch_mode<128, MODE>(a, units, mc, TM, s) : launch_mode<64, MODE>(a, units, mc, TM, s);
+int launch_hd(const PagedArgs &a, int hd, int units, int mc, Tiling t, hipStream_t s) {
+  if (t.wide) return paged_tile_launch(a, hd, MODE == PREFIX, units, mc, s);
+  return hd == 128 ? launch_mode<128, MODE>(a, units, mc, t.rows, s) : launch_mode<64, MODE>(a, units, mc, t.rows, s);
 }
 int merge(const PagedArgs &a, int hd, hipStream_t s) {
   if (a.MC == 1) return DCUT_OK;
@@ -416,19 +421,21 @@ int merge(const PagedArgs &a, int hd, hipStream_t s) {
 
 struct AttnPlan {
   Split own, pre;
-  int mc_own, mc_pre, units, tm, ptm;
+  Tiling tile, ptile;
+  int mc_own, mc_pre, units;
   size_t part, row_nc, total;
 };
 AttnPlan attn_plan(const dcut_paged_cfg *c, int B, bool shared) {
   AttnPlan p = {};
   const int G = c->n_q / c->n_kv;
-  p.tm = tile_rows((long long)G * c->max_block);
-  p.units = own_units(c, B);
-  p.own = paged_split((long long)p.units * c->n_kv, (long long)G * c->max_block <= p.tm);
+  const long long pairs = (long long)G * c->max_block;
+  p.tile = tiling(pairs);
+  p.units = pairs <= p.tile.rows ? B : (int)tile_bound(c->max_rows, G, p.tile.rows, B);
+  p.own = paged_split((long long)p.units * c->n_kv, p.tile.wide ? 512 : 2048, pairs <= p.tile.rows);
   p.mc_own = split_max(p.own, c->max_ctx);
   if (shared) {
-    p.ptm = tile_rows((long long)G * c->max_rows);
-    p.pre = paged_split(((long long)c->max_rows * G / p.ptm + 1) * c->n_kv, false);
+    p.ptile = tiling((long long)G * c->max_rows);
+    p.pre = paged_split(((long long)c->max_rows * G / p.ptile.rows + 1) * c->n_kv, p.ptile.wide ? 512 : 256, false);
     p.mc_pre = split_max(p.pre, c->max_ctx);
   }
   const int mc = p.mc_own + p.mc_pre;
@@ -443,10 +450,10 @@ AttnPlan attn_plan(const dcut_paged_cfg *c, int B, bool shared) {
 
 }  // namespace
 
-// Work items a launch aims for: about four for each of the three workgroups a CU holds, so that
-// ragged contexts even out.  Pieces under 128 keys cost more in partials than they win.
-Split paged_split(long long units, bool capped) {
-  long long S = (2048 + units - 1) / (units > 0 ? units : 1);
+// Pieces for a launch of about `items` work items.  Pieces under 128 keys cost more in partials
+// than they win.
+Split paged_split(long long units, int items, bool capped) {
+  long long S = (items + units - 1) / (units > 0 ? units : 1);
   if (S < 1) S = 1;
   if (S > 64) S = 64;
   return Split{(int)S, 128, capped ? 2048 : 1 << 30};
@@ -490,7 +497,7 @@ size_t paged_attn_ws_bytes(const dcut_paged_cfg *c, int B, bool shared) { return
 
 // Rows over their listed pages (a.list set, a.split, a.MC, a.part and a.row_nc too).
 int paged_list_attn_launch(const PagedArgs &a, int hd, hipStream_t s) {
-  DCUT_TRY(launch_hd<LIST>(a, hd, a.max_rows, a.MC, 64, s));
+  DCUT_TRY(launch_hd<LIST>(a, hd, a.max_rows, a.MC, Tiling{64, false}, s));
   return merge(a, hd, s);
 }
 
@@ -521,7 +528,7 @@ extern "C" int dcut_paged_attn(const dcut_paged_cfg *cfg, const dcut_pages *page
     a.part = (float *)((char *)ws + p.part);
     a.row_nc = (int32_t *)((char *)ws + p.row_nc);
   }
-  DCUT_TRY(launch_hd<OWN>(a, cfg->head_dim, p.units, p.mc_own, p.tm, stream));
+  DCUT_TRY(launch_hd<OWN>(a, cfg->head_dim, p.units, p.mc_own, p.tile, stream));
   return merge(a, cfg->head_dim, stream);
 }
 
@@ -544,8 +551,8 @@ extern "C" int dcut_paged_attn_shared(const dcut_paged_cfg *cfg, const dcut_page
   a.n_groups = n_groups;
   a.group_cu = group_cu;
   a.prefix_len = prefix_len;
-  const int punits = (int)tile_bound(cfg->max_rows, a.G, p.ptm, n_groups);
-  DCUT_TRY(launch_hd<PREFIX>(a, cfg->head_dim, punits, p.mc_pre, p.ptm, stream));
-  DCUT_TRY(launch_hd<OWN>(a, cfg->head_dim, p.units, p.mc_own, p.tm, stream));
+  const int punits = (int)tile_bound(cfg->max_rows, a.G, p.ptile.rows, n_groups);
+  DCUT_TRY(launch_hd<PREFIX>(a, cfg->head_dim, punits, p.mc_pre, p.ptile, stream));
+  DCUT_TRY(launch_hd<OWN>(a, cfg->head_dim, p.units, p.mc_own, p.tile, stream));
   return merge(a, cfg->head_dim, stream);
 }

@@ -201,7 +201,7 @@ SparsePlan sparse_plan(const dcut_paged_cfg *c, int n_sel) {
   SparsePlan p = {};
   const size_t rows = c->max_rows, tg = rows * c->n_kv;
   p.max_pages = (c->max_ctx + c->page - 1) / c->page;
-  p.split = paged_split((long long)rows * c->n_kv, false);
+  p.split = paged_split((long long)rows * c->n_kv, 2048, false);
   const long long most = (long long)n_sel * c->page;
   p.mc = split_max(p.split, (int)(most < c->max_ctx ? most : c->max_ctx));
   size_t off = 0;
