@@ -559,8 +559,8 @@ enum {
   DCUT_KERNEL_RS_FINISH,
   DCUT_KERNEL_ATTN_PLAN /* no kernel of its own: the attention work order is built by an extra
                            workgroup of the layer's first norm kernel */,
-  DCUT_KERNEL_PAGED_APPEND, DCUT_KERNEL_PAGED_BOUNDS, DCUT_KERNEL_PAGED_ATTN,
-  DCUT_KERNEL_PAGED_PREFIX, DCUT_KERNEL_PAGED_MERGE, DCUT_KERNEL_PAGE_SCORE, DCUT_KERNEL_PAGE_SELECT
+  DCUT_KERNEL_PAGED_APPEND, DCUT_KERNEL_PAGED_BOUNDS, DCUT_KERNEL_PAGED_PLAN, DCUT_KERNEL_PAGED_ATTN,
+  DCUT_KERNEL_PAGED_MERGE, DCUT_KERNEL_PAGE_SCORE, DCUT_KERNEL_PAGE_SELECT
 };
 int dcut_profile_arm(int kernel, hipEvent_t start, hipEvent_t stop);
 

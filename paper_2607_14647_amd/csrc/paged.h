@@ -11,6 +11,7 @@ namespace dcut {
 constexpr int PAGED_MAX_ROWS = 1 << 17;
 constexpr int PAGED_MAX_CTX = 1 << 24;
 constexpr int PAGED_MAX_GROUP = 64;       // query heads of a kv head
+constexpr int PLAN_HEAD = 256;
 
 // Key chunks of a row: a run of L keys is cut into pieces of chunk(L) keys, a multiple of 64,
 // at most S pieces unless they would pass cmax keys.  A function of L and of the launch's
@@ -44,6 +45,7 @@ struct PagedArgs {
   int MC;                     // partials a (row, head) may have
   float *part;                // [rows][n_q][MC][ATTN_PITCH(hd)]
   int32_t *row_nc;            // [rows] partials of the row's heads, 1: finished in place
+  int32_t *plan;              // work order of the requests' own items (PLAN_HEAD: count, items), or null
   // requests that share a prefix
   int n_groups;
   const int32_t *group_cu, *prefix_len;
@@ -88,9 +90,6 @@ Split paged_split(long long units, int items, bool capped);
 int split_max(const Split &s, int max_keys);
 PagedArgs paged_args(const dcut_paged_cfg *c, const dcut_pages *p, int B, const dcut_bf16 *q, long long ldq,
                      const int32_t *cu, const int32_t *ctx_len, dcut_bf16 *out, float *lse, int32_t *dev_err);
-// Units of many rows (paged_tile.hip): rows of a tile, the launch.
-int paged_tile_rows();
-int paged_tile_launch(const PagedArgs &a, int head_dim, bool prefix, int units, int mc, hipStream_t s);
 int paged_list_attn_launch(const PagedArgs &a, int head_dim, hipStream_t s);
 size_t paged_attn_ws_bytes(const dcut_paged_cfg *c, int B, bool shared);
 size_t paged_sparse_ws_bytes(const dcut_paged_cfg *c, int n_sel);

@@ -110,43 +110,60 @@ k_paged_append(AppendArgs a) {
   }
 }
 
-// Channel bounds of the pages that the appended rows filled: the workgroup of (row, kv head)
-// whose row took its page's last slot reads the page's keys, 8 channels and every
-// (256 / (HD / 8))-th key a thread, and joins the threads of a channel in LDS.
+// Channel bounds of the pages that the appended rows filled.  A workgroup looks through 16 rows
+// (no page is smaller) for one kv head; for each that took its page's last slot it reads the
+// page's keys, 8 channels and every (256 / (HD / 8))-th key a thread, and joins the threads of
+// a channel in LDS.
+constexpr int BOUND_ROWS = 16;
+
 template <int HD>
 __global__ void __launch_bounds__(256)
 k_page_bounds(AppendArgs a, uint16_t *kmin, uint16_t *kmax) {
   constexpr int CH = HD / 8, KS = 256 / CH;
   __shared__ float s_lo[KS][HD], s_hi[KS][HD];
-  const int t = blockIdx.x, g = blockIdx.y;
+  __shared__ int s_page[BOUND_ROWS];        // pool page that the row filled, or -1
+  const int g = blockIdx.y, t0 = blockIdx.x * BOUND_ROWS;
   const int M = min(a.cu[a.B], a.max_rows);
   const int page = 1 << a.lpage;
-  if (t >= M) return;
-  const int p = a.pos[t], i = a.req[t];
-  if ((p & (page - 1)) != page - 1) return;
-  if (i < 0 || i >= a.B || p < 0 || p >= a.max_ctx || (p >> a.lpage) >= a.table_ld) return;
-  const int pg = a.table[(size_t)i * a.table_ld + (p >> a.lpage)];
-  if ((unsigned)pg >= (unsigned)a.n_pages) return;
-  const int c = threadIdx.x % CH, k0 = threadIdx.x / CH;
-  const uint16_t *src = a.pk + ((size_t)pg * a.n_kv + g) * (size_t)page * HD + 8 * c;
-  float lo[8], hi[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) { lo[j] = __builtin_inff(); hi[j] = -__builtin_inff(); }
-  for (int k = k0; k < page; k += KS) {
-    float x[8];
-    load8(src + (size_t)k * HD, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) { lo[j] = fminf(lo[j], x[j]); hi[j] = fmaxf(hi[j], x[j]); }
+  if (t0 >= M) return;
+  if (threadIdx.x < BOUND_ROWS) {
+    const int t = t0 + threadIdx.x;
+    int pg = -1;
+    if (t < M) {
+      const int p = a.pos[t], i = a.req[t];
+      if ((p & (page - 1)) == page - 1 && i >= 0 && i < a.B && p >= 0 && p < a.max_ctx && (p >> a.lpage) < a.table_ld) {
+        pg = a.table[(size_t)i * a.table_ld + (p >> a.lpage)];
+        if ((unsigned)pg >= (unsigned)a.n_pages) pg = -1;
+      }
+    }
+    s_page[threadIdx.x] = pg;
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) { s_lo[k0][8 * c + j] = lo[j]; s_hi[k0][8 * c + j] = hi[j]; }
   __syncthreads();
-  if (threadIdx.x < HD) {
-    float l = s_lo[0][threadIdx.x], h = s_hi[0][threadIdx.x];
-    for (int k = 1; k < KS; ++k) { l = fminf(l, s_lo[k][threadIdx.x]); h = fmaxf(h, s_hi[k][threadIdx.x]); }
-    const size_t o = ((size_t)pg * a.n_kv + g) * HD + threadIdx.x;
-    kmin[o] = f2bf(l);
-    kmax[o] = f2bf(h);
+  const int c = threadIdx.x % CH, k0 = threadIdx.x / CH;
+  for (int e = 0; e < BOUND_ROWS; ++e) {
+    const int pg = s_page[e];
+    if (pg < 0) continue;                   // uniform
+    const uint16_t *src = a.pk + ((size_t)pg * a.n_kv + g) * (size_t)page * HD + 8 * c;
+    float lo[8], hi[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { lo[j] = __builtin_inff(); hi[j] = -__builtin_inff(); }
+    for (int k = k0; k < page; k += KS) {
+      float x[8];
+      load8(src + (size_t)k * HD, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { lo[j] = fminf(lo[j], x[j]); hi[j] = fmaxf(hi[j], x[j]); }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { s_lo[k0][8 * c + j] = lo[j]; s_hi[k0][8 * c + j] = hi[j]; }
+    __syncthreads();
+    if (threadIdx.x < HD) {
+      float l = s_lo[0][threadIdx.x], h = s_hi[0][threadIdx.x];
+      for (int k = 1; k < KS; ++k) { l = fminf(l, s_lo[k][threadIdx.x]); h = fmaxf(h, s_hi[k][threadIdx.x]); }
+      const size_t o = ((size_t)pg * a.n_kv + g) * HD + threadIdx.x;
+      kmin[o] = f2bf(l);
+      kmax[o] = f2bf(h);
+    }
+    __syncthreads();
   }
 }
 
@@ -156,7 +173,7 @@ int append_launch(const AppendArgs &a, const dcut_pages *pg, hipStream_t s) {
   DCUT_TRY(launch(DCUT_KERNEL_PAGED_APPEND, k_paged_append<HD, T, ROWS>, dim3((a.max_rows + ROWS - 1) / ROWS), dim3(256), 0,
                   s, a));
   if (!pg->kmin) return DCUT_OK;
-  return launch(DCUT_KERNEL_PAGED_BOUNDS, k_page_bounds<HD>, dim3(a.max_rows, a.n_kv), dim3(256), 0, s, a, pg->kmin, pg->kmax);
+  return launch(DCUT_KERNEL_PAGED_BOUNDS, k_page_bounds<HD>, dim3((a.max_rows + BOUND_ROWS - 1) / BOUND_ROWS, a.n_kv), dim3(256), 0, s, a, pg->kmin, pg->kmax);
 }
 
 }  // namespace

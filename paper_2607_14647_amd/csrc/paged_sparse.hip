@@ -23,35 +23,24 @@ struct SparseArgs {
 };
 
 // A row's request and position, by counting the requests that start at or before it.
+template <int THREADS>
 __device__ __forceinline__ int request_of(const PagedArgs &a, int t, int *s_cnt) {
   int cnt = 0;
-  for (int j = threadIdx.x; j < a.B; j += 256) cnt += a.cu[j + 1] <= t;
+  for (int j = threadIdx.x; j < a.B; j += THREADS) cnt += a.cu[j + 1] <= t;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) cnt += __shfl_xor(cnt, off, 64);
   if ((threadIdx.x & 63) == 0) s_cnt[threadIdx.x >> 6] = cnt;
   __syncthreads();
-  cnt = s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3];
+  cnt = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) cnt += s_cnt[w];
   __syncthreads();
   return cnt;
 }
 
-// Scores of 256 pages of one (row, kv head): a page a thread, which reads its page's bounds
-// 16 bytes at a time; the group's sums a and b come from LDS.
+// The group's sums of one (row, kv head), by the first HD threads of the workgroup.
 template <int HD>
-__global__ void __launch_bounds__(256)
-k_page_score(SparseArgs s) {
-  const PagedArgs &a = s.p;
-  __shared__ double s_a[HD], s_b[HD];
-  __shared__ int s_cnt[4];
-  const int t = blockIdx.x, g = blockIdx.y;
-  if (t >= a.cu[a.B] || t >= a.max_rows) return;
-  const int i = request_of(a, t, s_cnt);
-  ReqRows r;
-  if (i >= a.B || !paged_request(a, i, false, r)) return;
-  const int pos = r.L + t - r.t0;
-  const int last = pos >> a.lpage;
-  const int j = blockIdx.z * 256 + threadIdx.x;
-  if ((int)(blockIdx.z * 256) > last || last < s.n_sel) return;     // all of its pages are read
+__device__ __forceinline__ void group_sums(const PagedArgs &a, int t, int g, double *s_a, double *s_b) {
   if (threadIdx.x < HD) {
     double p = 0.0, n = 0.0;
     for (int h = 0; h < a.G; ++h) {
@@ -62,21 +51,69 @@ k_page_score(SparseArgs s) {
     s_a[threadIdx.x] = p;
     s_b[threadIdx.x] = n;
   }
-  __syncthreads();
-  if (j > last) return;
-  const int pg = a.table[(size_t)i * a.table_ld + j];
-  const size_t row = ((size_t)((unsigned)pg < (unsigned)a.n_pages ? pg : 0) * a.n_kv + g) * HD;
-  double acc = 0.0;
-  for (int d = 0; d < HD; d += 8) {
-    const uint4 hi = *(const uint4 *)(s.kmax + row + d), lo = *(const uint4 *)(s.kmin + row + d);
-    const uint16_t *eh = (const uint16_t *)&hi, *el = (const uint16_t *)&lo;
+}
+
+// Scores of pages j0 .. j1-1 of one (row, kv head), eight lanes a page: each reads an eighth of
+// its page's bounds at once and keeps its eighth of the sums in registers.
+template <int HD, int THREADS, typename Store>
+__device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *table, int g, int j0, int j1,
+                                            const double *s_a, const double *s_b, Store store) {
+  constexpr int Q = HD / 8;
+  const PagedArgs &a = s.p;
+  const int c = threadIdx.x & 7;
+  double av[Q], bv[Q];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      acc = fma(s_a[d + u], (double)bf2f(eh[u]), acc);
-      acc = fma(s_b[d + u], (double)bf2f(el[u]), acc);
-    }
+  for (int d = 0; d < Q; ++d) {
+    av[d] = s_a[c * Q + d];
+    bv[d] = s_b[c * Q + d];
   }
-  s.score[((size_t)t * a.n_kv + g) * s.max_pages + j] = acc;
+  for (int j = j0 + (threadIdx.x >> 3); j < j1; j += THREADS / 8) {
+    const int pg = table[j];
+    const size_t row = ((size_t)((unsigned)pg < (unsigned)a.n_pages ? pg : 0) * a.n_kv + g) * HD + c * Q;
+    uint4 hi[Q / 8], lo[Q / 8];
+#pragma unroll
+    for (int e = 0; e < Q / 8; ++e) {
+      hi[e] = *(const uint4 *)(s.kmax + row + 8 * e);
+      lo[e] = *(const uint4 *)(s.kmin + row + 8 * e);
+    }
+    double acc = 0.0;
+#pragma unroll
+    for (int e = 0; e < Q / 8; ++e) {
+      const uint16_t *eh = (const uint16_t *)&hi[e], *el = (const uint16_t *)&lo[e];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        acc = fma(av[8 * e + u], (double)bf2f(eh[u]), acc);
+        acc = fma(bv[8 * e + u], (double)bf2f(el[u]), acc);
+      }
+    }
+    acc += __shfl_xor(acc, 1, 64);
+    acc += __shfl_xor(acc, 2, 64);
+    acc += __shfl_xor(acc, 4, 64);
+    if (c == 0) store(j, acc);
+  }
+}
+
+constexpr int SCORE_PAGES = 128;      // pages a workgroup of k_page_score
+
+template <int HD>
+__global__ void __launch_bounds__(256)
+k_page_score(SparseArgs s) {
+  const PagedArgs &a = s.p;
+  __shared__ double s_a[HD], s_b[HD];
+  __shared__ int s_cnt[4];
+  const int t = blockIdx.x, g = blockIdx.y;
+  if (t >= a.cu[a.B] || t >= a.max_rows) return;
+  const int i = request_of<256>(a, t, s_cnt);
+  ReqRows r;
+  if (i >= a.B || !paged_request(a, i, false, r)) return;
+  const int last = (r.L + t - r.t0) >> a.lpage;
+  const int j0 = blockIdx.z * SCORE_PAGES;
+  if (j0 > last || last < s.n_sel) return;                          // all of its pages are read
+  group_sums<HD>(a, t, g, s_a, s_b);
+  __syncthreads();
+  double *score = s.score + ((size_t)t * a.n_kv + g) * s.max_pages;
+  score_pages<HD, 256>(s, a.table + (size_t)i * a.table_ld, g, j0, min(j0 + SCORE_PAGES, last + 1), s_a, s_b,
+                  [&](int j, double x) { score[j] = x; });
 }
 
 // Unsigned keys in the order of the scores, NaN below every number.
@@ -86,17 +123,26 @@ __device__ __forceinline__ unsigned long long order_key(double x) {
   return (u >> 63) ? ~u : u | 0x8000000000000000ull;
 }
 
+constexpr int FUSED_PAGES = 1024;     // pages up to which one workgroup scores and selects
+
 // The n_sel pages of one (row, kv head): the first n_sink and the last n_local, then by score,
-// ties to the lower page.  A radix select finds the score of the last page taken; pages above
-// it, and the lowest ones equal to it, are listed in ascending order by a scan.
-__global__ void __launch_bounds__(256)
+// ties to the lower page.  Each thread owns a run of pages.  A radix select over the scores'
+// bits, from the highest that differs, finds the score of the last page taken; the pages
+// above it, and the lowest ones equal to it, are listed in ascending order by one scan.
+// NK: pages a thread keeps in registers, 0: any number, read again in every round.
+constexpr int ST = 1024;              // threads of k_page_select
+
+template <int HD, bool FUSED, int NK>
+__global__ void __launch_bounds__(ST)
 k_page_select(SparseArgs s) {
   const PagedArgs &a = s.p;
-  __shared__ int s_cnt[4], s_hist[256], s_pick[2];
+  __shared__ double s_a[FUSED ? HD : 1], s_b[FUSED ? HD : 1], s_score[FUSED ? FUSED_PAGES : 1];
+  __shared__ int s_cnt[ST / 64], s_hist[2][256], s_pick[2], s_eq[ST / 64], s_gt[ST / 64];
+  __shared__ unsigned long long s_diff[ST / 64];
   const int t = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
   if (t >= a.cu[a.B] || t >= a.max_rows) return;
   const size_t tg = (size_t)t * a.n_kv + g;
-  const int i = request_of(a, t, s_cnt);
+  const int i = request_of<ST>(a, t, s_cnt);
   ReqRows r;
   if (i >= a.B || !paged_request(a, i, g == 0 && tid == 0, r)) {
     if (tid == 0) s.list_keys[tg] = 0;
@@ -110,33 +156,65 @@ k_page_select(SparseArgs s) {
   const int n = min(np, s.n_sel);
   if (tid == 0) s.list_keys[tg] = (n - 1) * a.page + (pos & (a.page - 1)) + 1;
   if (np <= s.n_sel) {
-    for (int j = tid; j < s.n_sel; j += 256) {
+    for (int j = tid; j < s.n_sel; j += ST) {
       if (j < np) list[j] = table[j];
       if (blocks) blocks[j] = j < np ? j : -1;
     }
     return;
   }
-  const double *score = s.score + tg * s.max_pages;
-  auto key = [&](int j) {
-    if (j < s.n_sink || j > last - s.n_local) return ~0ull;
-    return order_key(score[j]);
-  };
-  // the n-th largest key: eight bits a round
-  unsigned long long prefix = 0;
-  int need = n;
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    s_hist[tid] = 0;
+  const double *score = FUSED ? s_score : s.score + tg * s.max_pages;
+  if (FUSED) {
+    group_sums<HD>(a, t, g, s_a, s_b);
     __syncthreads();
-    const unsigned long long mask = shift == 56 ? 0 : ~0ull << (shift + 8);
-    for (int j = tid; j < np; j += 256) {
-      const unsigned long long k = key(j);
-      if ((k & mask) == prefix) atomicAdd(&s_hist[(int)(k >> shift) & 255], 1);
+    score_pages<HD, ST>(s, table, g, 0, np, s_a, s_b, [&](int j, double x) { s_score[j] = x; });
+    __syncthreads();
+  }
+  const int local = np - s.n_local;         // pages from here on and those below n_sink are taken in any case
+  const int per = NK ? NK : (np + ST - 1) / ST;
+  const int j0 = tid * per;
+  // a forced page has key 0, which no score has, and is no candidate
+  auto read = [&](int j) { return j < s.n_sink || j >= local ? 0ull : order_key(score[j]); };
+  unsigned long long kreg[NK ? NK : 1];
+  if (NK) {
+#pragma unroll
+    for (int e = 0; e < NK; ++e) kreg[e] = read(j0 + e);
+  }
+  auto each = [&](auto f) {
+    if (NK) {
+#pragma unroll
+      for (int e = 0; e < NK; ++e) f(e, kreg[NK ? e : 0]);
+    } else {
+      for (int e = 0; e < per; ++e) f(e, read(j0 + e));
     }
+  };
+  // the highest bit in which two candidates differ
+  const unsigned long long first = read(min(s.n_sink, local - 1));          // a candidate: np > n_sel >= n_sink + n_local
+  unsigned long long diff = 0;
+  each([&](int, unsigned long long k) { diff |= k ? k ^ first : 0; });
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) diff |= __shfl_xor(diff, off, 64);
+  if ((tid & 63) == 0) s_diff[tid >> 6] = diff;
+  if (tid < 256) s_hist[0][tid] = 0;
+  __syncthreads();
+  diff = 0;
+#pragma unroll
+  for (int w = 0; w < ST / 64; ++w) diff |= s_diff[w];
+  const int top = 64 - __clzll((long long)diff);                            // bits from `top` on are common
+  unsigned long long mask = top >= 64 ? 0 : ~0ull << top, prefix = first & mask;
+  int need = n - min(s.n_sink, np) - min(s.n_local, np);                    // np > n_sel: sinks and locals are apart
+  int lo = top;                                                             // bits below lo are open
+  for (int round = 0; lo > 0 && need > 0; ++round) {
+    const int bits = lo < 8 ? lo : 8, shift = lo - bits;
+    int *hist = s_hist[round & 1];
+    each([&](int, unsigned long long k) {
+      if (k && (k & mask) == prefix) atomicAdd(&hist[(int)(k >> shift) & ((1 << bits) - 1)], 1);
+    });
+    if (tid < 256) s_hist[(round + 1) & 1][tid] = 0;
     __syncthreads();
     if (tid < 64) {                         // digits from the largest: four a lane
       int c[4], sum = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { c[e] = s_hist[255 - 4 * tid - e]; sum += c[e]; }
+      for (int e = 0; e < 4; ++e) { c[e] = hist[255 - 4 * tid - e]; sum += c[e]; }
       int x = sum;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -146,50 +224,62 @@ k_page_select(SparseArgs s) {
       int before = x - sum;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (before < need && need <= before + c[e]) { s_pick[0] = 255 - 4 * tid - e; s_pick[1] = need - before; }
+        if (before < need && need <= before + c[e]) {
+          s_pick[0] = (255 - 4 * tid - e) | (need - before == c[e] ? 256 : 0);
+          s_pick[1] = need - before;
+        }
         before += c[e];
       }
     }
     __syncthreads();
-    prefix |= (unsigned long long)s_pick[0] << shift;
+    const int pick = s_pick[0];
+    mask |= (unsigned long long)((1 << bits) - 1) << shift;
+    prefix |= (unsigned long long)(pick & 255) << shift;
     need = s_pick[1];
-    __syncthreads();
+    lo = shift;
+    if (pick & 256) break;                  // every key of this prefix is taken
   }
-  // need: how many of the keys equal to `prefix` are taken, the lowest pages first
-  int taken = 0, equal = 0;
-  for (int j0 = 0; j0 < np; j0 += 256) {
-    const int j = j0 + tid;
-    const unsigned long long k = j < np ? key(j) : 0;
-    const int eq = j < np && k == prefix, gt = j < np && k > prefix;
-    // ranks of this thread among the equal and the taken ones
-    int v = eq | (gt << 16);
-    int x = v;
+  // of the keys with this prefix, `need` are taken, the lowest pages first
+  int eq = 0, gt = 0;
+  each([&](int e, unsigned long long k) {
+    const int j = j0 + e;
+    gt += j < np && (k == 0 || (k & mask) > prefix);
+    eq += j < np && k && (k & mask) == prefix;
+  });
+  int xe = eq, xg = gt;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x, o, 64);
-      if ((tid & 63) >= o) x += y;
-    }
-    if ((tid & 63) == 63) s_cnt[tid >> 6] = x;
-    __syncthreads();
-    int before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if (w < (tid >> 6)) before += s_cnt[w];
-      total += s_cnt[w];
-    }
-    x += before - v;                         // exclusive
-    const int eq_rank = equal + (x & 0xffff), gt_rank = x >> 16;
-    const int eq_before = min(eq_rank, need) - min(equal, need);
-    if (gt || (eq && eq_rank < need)) {
-      const int at = taken + gt_rank + eq_before;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int ye = __shfl_up(xe, o, 64), yg = __shfl_up(xg, o, 64);
+    if ((tid & 63) >= o) { xe += ye; xg += yg; }
+  }
+  if ((tid & 63) == 63) { s_eq[tid >> 6] = xe; s_gt[tid >> 6] = xg; }
+  __syncthreads();
+  xe -= eq;
+  xg -= gt;
+  for (int w = 0; w < (tid >> 6); ++w) { xe += s_eq[w]; xg += s_gt[w]; }
+  each([&](int e, unsigned long long k) {
+    const int j = j0 + e;
+    if (j >= np) return;
+    const bool is_gt = k == 0 || (k & mask) > prefix, is_eq = k && (k & mask) == prefix;
+    if (is_gt || (is_eq && xe < need)) {
+      const int at = xg + min(xe, need);
       list[at] = table[j];
       if (blocks) blocks[at] = j;
     }
-    const int eq_all = total & 0xffff, gt_all = total >> 16;
-    taken += gt_all + min(equal + eq_all, need) - min(equal, need);
-    equal += eq_all;
-    __syncthreads();
-  }
+    xg += is_gt;
+    xe += is_eq;
+  });
+}
+
+template <int HD>
+int select_launch(const SparseArgs &s, dim3 grid, hipStream_t st) {
+  if (s.max_pages <= s.n_sel || s.max_pages <= FUSED_PAGES)
+    return launch(DCUT_KERNEL_PAGE_SELECT, k_page_select<HD, true, (FUSED_PAGES + ST - 1) / ST>, grid, dim3(ST), 0, st, s);
+  const dim3 sgrid(grid.x, grid.y, (s.max_pages + SCORE_PAGES - 1) / SCORE_PAGES);
+  DCUT_TRY(launch(DCUT_KERNEL_PAGE_SCORE, k_page_score<HD>, sgrid, dim3(256), 0, st, s));
+  if (s.max_pages <= 4 * ST)
+    return launch(DCUT_KERNEL_PAGE_SELECT, k_page_select<HD, false, 4>, grid, dim3(ST), 0, st, s);
+  return launch(DCUT_KERNEL_PAGE_SELECT, k_page_select<HD, false, 0>, grid, dim3(ST), 0, st, s);
 }
 
 struct SparsePlan {
@@ -201,11 +291,11 @@ SparsePlan sparse_plan(const dcut_paged_cfg *c, int n_sel) {
   SparsePlan p = {};
   const size_t rows = c->max_rows, tg = rows * c->n_kv;
   p.max_pages = (c->max_ctx + c->page - 1) / c->page;
-  p.split = paged_split((long long)rows * c->n_kv, 2048, false);
+  p.split = paged_split((long long)rows * c->n_kv, 1024, false);
   const long long most = (long long)n_sel * c->page;
   p.mc = split_max(p.split, (int)(most < c->max_ctx ? most : c->max_ctx));
   size_t off = 0;
-  p.score = off; off = align256(off + (p.max_pages > n_sel ? tg * p.max_pages * sizeof(double) : 0));
+  p.score = off; off = align256(off + (p.max_pages > n_sel && p.max_pages > FUSED_PAGES ? tg * p.max_pages * sizeof(double) : 0));
   p.list = off; off = align256(off + tg * n_sel * sizeof(int32_t));
   p.keys = off; off = align256(off + tg * sizeof(int32_t));
   p.part = off;
@@ -251,13 +341,7 @@ extern "C" int dcut_paged_attn_sparse(const dcut_paged_cfg *cfg, const dcut_page
     s.p.part = (float *)((char *)ws + p.part);
     s.p.row_nc = (int32_t *)((char *)ws + p.row_nc);
   }
-  if (p.max_pages > n_sel) {
-    const dim3 grid(cfg->max_rows, cfg->n_kv, (p.max_pages + 255) / 256);
-    if (cfg->head_dim == 128)
-      DCUT_TRY(launch(DCUT_KERNEL_PAGE_SCORE, k_page_score<128>, grid, dim3(256), 0, stream, s));
-    else
-      DCUT_TRY(launch(DCUT_KERNEL_PAGE_SCORE, k_page_score<64>, grid, dim3(256), 0, stream, s));
-  }
-  DCUT_TRY(launch(DCUT_KERNEL_PAGE_SELECT, k_page_select, dim3(cfg->max_rows, cfg->n_kv), dim3(256), 0, stream, s));
+  const dim3 grid(cfg->max_rows, cfg->n_kv);
+  DCUT_TRY(cfg->head_dim == 128 ? select_launch<128>(s, grid, stream) : select_launch<64>(s, grid, stream));
   return paged_list_attn_launch(s.p, cfg->head_dim, stream);
 }

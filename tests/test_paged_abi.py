@@ -101,7 +101,8 @@ def test_workspaces_are_checked():
     # the partial sums do not grow without bound with the context: at most one per 2048 keys
     # once a request has more than its share of pieces
     big = _cfg(max_ctx=1 << 20, max_rows=512, n_q=32, n_kv=8)
-    assert L.paged_workspace_bytes("attn", big, 512) <= 512 * 32 * 512 * 132 * 4 + 4096
+    # (132 float32 each), and a work order of one 16-byte entry per request and piece
+    assert L.paged_workspace_bytes("attn", big, 512) <= 512 * 32 * 512 * 132 * 4 + 512 * 512 * 16 + 4096
 
 
 def test_oracle_closed_forms():
