@@ -73,6 +73,10 @@ __device__ __forceinline__ bool paged_request(const PagedArgs &a, int i, bool re
   return ok;
 }
 
+// A value, a condition, that every lane finds alike, in a scalar register.
+__device__ __forceinline__ int uniform_int(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ bool uniform_if(bool x) { return uniform_int(x) != 0; }
+
 // Uniform loads from arrays that no kernel of the call writes: one scalar load instead of a
 // vector load, whose wait would drain the operand stream in flight.
 typedef __attribute__((address_space(4))) const int32_t const_i32;

@@ -33,10 +33,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void *base,
   return __builtin_amdgcn_make_buffer_rsrc((void *)(((uintptr_t)hi << 32) | lo), (short)0, bytes, 0x00020000);
 }
 
-// A value, a condition, that every lane finds alike, in a scalar register.
-__device__ __forceinline__ int uniform_int(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ bool uniform_if(bool x) { return uniform_int(x) != 0; }
-
 enum Mode { OWN = 0, PREFIX = 1, LIST = 2 };
 
 // What a work item reads and computes; uniform over the workgroup.

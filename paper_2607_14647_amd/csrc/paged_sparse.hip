@@ -22,20 +22,29 @@ struct SparseArgs {
   int32_t *blocks;            // [rows][n_kv][n_sel] or null
 };
 
-// A row's request and position, by counting the requests that start at or before it.
+// A row's request and where it sits, found by all threads: the one that holds the request's
+// bounds passes them on.  False (for all) where the row is not live or its request is refused.
+struct RowAt {
+  int i, pos;
+};
 template <int THREADS>
-__device__ __forceinline__ int request_of(const PagedArgs &a, int t, int *s_cnt) {
-  int cnt = 0;
-  for (int j = threadIdx.x; j < a.B; j += THREADS) cnt += a.cu[j + 1] <= t;
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) cnt += __shfl_xor(cnt, off, 64);
-  if ((threadIdx.x & 63) == 0) s_cnt[threadIdx.x >> 6] = cnt;
+__device__ __forceinline__ bool find_row(const PagedArgs &a, int t, int *s_row, bool report, RowAt &row) {
+  if (threadIdx.x == 0) s_row[0] = -1;
   __syncthreads();
-  cnt = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) cnt += s_cnt[w];
+  for (int j = threadIdx.x; j < a.B; j += THREADS) {
+    const int lo = a.cu[j], hi = a.cu[j + 1], L = a.ctx_len[j];
+    if (lo <= t && t < hi) {
+      ReqRows r;
+      if (t < a.max_rows && t < a.cu[a.B] && paged_request(a, j, report, r)) {
+        s_row[1] = L + t - lo;
+        s_row[0] = j;
+      }
+    }
+  }
   __syncthreads();
-  return cnt;
+  row.i = uniform_int(s_row[0]);
+  row.pos = uniform_int(s_row[1]);
+  return row.i >= 0;
 }
 
 // The group's sums of one (row, kv head), by the first HD threads of the workgroup.
@@ -43,10 +52,12 @@ template <int HD>
 __device__ __forceinline__ void group_sums(const PagedArgs &a, int t, int g, double *s_a, double *s_b) {
   if (threadIdx.x < HD) {
     double p = 0.0, n = 0.0;
+    const uint16_t *q = a.q + (size_t)t * a.ldq + (size_t)g * a.G * HD + threadIdx.x;
+#pragma unroll 4
     for (int h = 0; h < a.G; ++h) {
-      const float q = bf2f(a.q[(size_t)t * a.ldq + (size_t)(g * a.G + h) * HD + threadIdx.x]);
-      p += (double)fmaxf(q, 0.0f);
-      n += (double)fminf(q, 0.0f);
+      const float x = bf2f(q[h * HD]);
+      p += (double)fmaxf(x, 0.0f);
+      n += (double)fminf(x, 0.0f);
     }
     s_a[threadIdx.x] = p;
     s_b[threadIdx.x] = n;
@@ -54,11 +65,12 @@ __device__ __forceinline__ void group_sums(const PagedArgs &a, int t, int g, dou
 }
 
 // Scores of pages j0 .. j1-1 of one (row, kv head), eight lanes a page: each reads an eighth of
-// its page's bounds at once and keeps its eighth of the sums in registers.
-template <int HD, int THREADS, typename Store>
+// its page's bounds at once and keeps its eighth of the sums in registers.  The bounds of U
+// pages a lane are asked for together: a page is 512 bytes at a random place.
+template <int HD, int THREADS, int U, typename Store>
 __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *table, int g, int j0, int j1,
                                             const double *s_a, const double *s_b, Store store) {
-  constexpr int Q = HD / 8;
+  constexpr int Q = HD / 8, STEP = THREADS / 8;
   const PagedArgs &a = s.p;
   const int c = threadIdx.x & 7;
   double av[Q], bv[Q];
@@ -67,52 +79,58 @@ __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *
     av[d] = s_a[c * Q + d];
     bv[d] = s_b[c * Q + d];
   }
-  for (int j = j0 + (threadIdx.x >> 3); j < j1; j += THREADS / 8) {
-    const int pg = table[j];
-    const size_t row = ((size_t)((unsigned)pg < (unsigned)a.n_pages ? pg : 0) * a.n_kv + g) * HD + c * Q;
-    uint4 hi[Q / 8], lo[Q / 8];
+  for (int j = j0 + (threadIdx.x >> 3); j < j1; j += U * STEP) {
+    int pg[U];
 #pragma unroll
-    for (int e = 0; e < Q / 8; ++e) {
-      hi[e] = *(const uint4 *)(s.kmax + row + 8 * e);
-      lo[e] = *(const uint4 *)(s.kmin + row + 8 * e);
-    }
-    double acc = 0.0;
+    for (int u = 0; u < U; ++u) pg[u] = table[min(j + u * STEP, j1 - 1)];
+    uint4 hi[U][Q / 8], lo[U][Q / 8];
 #pragma unroll
-    for (int e = 0; e < Q / 8; ++e) {
-      const uint16_t *eh = (const uint16_t *)&hi[e], *el = (const uint16_t *)&lo[e];
+    for (int u = 0; u < U; ++u) {
+      const size_t row = ((size_t)((unsigned)pg[u] < (unsigned)a.n_pages ? pg[u] : 0) * a.n_kv + g) * HD + c * Q;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        acc = fma(av[8 * e + u], (double)bf2f(eh[u]), acc);
-        acc = fma(bv[8 * e + u], (double)bf2f(el[u]), acc);
+      for (int e = 0; e < Q / 8; ++e) {
+        hi[u][e] = *(const uint4 *)(s.kmax + row + 8 * e);
+        lo[u][e] = *(const uint4 *)(s.kmin + row + 8 * e);
       }
     }
-    acc += __shfl_xor(acc, 1, 64);
-    acc += __shfl_xor(acc, 2, 64);
-    acc += __shfl_xor(acc, 4, 64);
-    if (c == 0) store(j, acc);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      double acc = 0.0;
+#pragma unroll
+      for (int e = 0; e < Q / 8; ++e) {
+        const uint16_t *eh = (const uint16_t *)&hi[u][e], *el = (const uint16_t *)&lo[u][e];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          acc = fma(av[8 * e + w], (double)bf2f(eh[w]), acc);
+          acc = fma(bv[8 * e + w], (double)bf2f(el[w]), acc);
+        }
+      }
+      acc += __shfl_xor(acc, 1, 64);
+      acc += __shfl_xor(acc, 2, 64);
+      acc += __shfl_xor(acc, 4, 64);
+      if (c == 0 && j + u * STEP < j1) store(j + u * STEP, acc);
+    }
   }
 }
 
-constexpr int SCORE_PAGES = 128;      // pages a workgroup of k_page_score
+constexpr int SCORE_PAGES = 256;      // pages a workgroup of k_page_score takes
 
 template <int HD>
 __global__ void __launch_bounds__(256)
 k_page_score(SparseArgs s) {
   const PagedArgs &a = s.p;
   __shared__ double s_a[HD], s_b[HD];
-  __shared__ int s_cnt[4];
+  __shared__ int s_row[2];
   const int t = blockIdx.x, g = blockIdx.y;
-  if (t >= a.cu[a.B] || t >= a.max_rows) return;
-  const int i = request_of<256>(a, t, s_cnt);
-  ReqRows r;
-  if (i >= a.B || !paged_request(a, i, false, r)) return;
-  const int last = (r.L + t - r.t0) >> a.lpage;
+  RowAt row;
+  if (!find_row<256>(a, t, s_row, false, row)) return;
+  const int last = row.pos >> a.lpage;
   const int j0 = blockIdx.z * SCORE_PAGES;
   if (j0 > last || last < s.n_sel) return;                          // all of its pages are read
   group_sums<HD>(a, t, g, s_a, s_b);
   __syncthreads();
   double *score = s.score + ((size_t)t * a.n_kv + g) * s.max_pages;
-  score_pages<HD, 256>(s, a.table + (size_t)i * a.table_ld, g, j0, min(j0 + SCORE_PAGES, last + 1), s_a, s_b,
+  score_pages<HD, 256, 2>(s, a.table + (size_t)row.i * a.table_ld, g, j0, min(j0 + SCORE_PAGES, last + 1), s_a, s_b,
                   [&](int j, double x) { score[j] = x; });
 }
 
@@ -137,20 +155,18 @@ __global__ void __launch_bounds__(ST)
 k_page_select(SparseArgs s) {
   const PagedArgs &a = s.p;
   __shared__ double s_a[FUSED ? HD : 1], s_b[FUSED ? HD : 1], s_score[FUSED ? FUSED_PAGES : 1];
-  __shared__ int s_cnt[ST / 64], s_hist[2][256], s_pick[2], s_eq[ST / 64], s_gt[ST / 64];
+  __shared__ int s_row[2], s_hist[2][256], s_pick[2], s_eq[ST / 64], s_gt[ST / 64];
   __shared__ unsigned long long s_diff[ST / 64];
   const int t = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
-  if (t >= a.cu[a.B] || t >= a.max_rows) return;
   const size_t tg = (size_t)t * a.n_kv + g;
-  const int i = request_of<ST>(a, t, s_cnt);
-  ReqRows r;
-  if (i >= a.B || !paged_request(a, i, g == 0 && tid == 0, r)) {
+  RowAt row;
+  if (!find_row<ST>(a, t, s_row, g == 0, row)) {
     if (tid == 0) s.list_keys[tg] = 0;
     return;
   }
-  const int pos = r.L + t - r.t0;
+  const int pos = row.pos;
   const int last = pos >> a.lpage, np = last + 1;
-  const int32_t *table = a.table + (size_t)i * a.table_ld;
+  const int32_t *table = a.table + (size_t)row.i * a.table_ld;
   int32_t *list = s.list + tg * s.n_sel;
   int32_t *blocks = s.blocks ? s.blocks + tg * s.n_sel : nullptr;
   const int n = min(np, s.n_sel);
@@ -166,7 +182,7 @@ k_page_select(SparseArgs s) {
   if (FUSED) {
     group_sums<HD>(a, t, g, s_a, s_b);
     __syncthreads();
-    score_pages<HD, ST>(s, table, g, 0, np, s_a, s_b, [&](int j, double x) { s_score[j] = x; });
+    score_pages<HD, ST, 2>(s, table, g, 0, np, s_a, s_b, [&](int j, double x) { s_score[j] = x; });
     __syncthreads();
   }
   const int local = np - s.n_local;         // pages from here on and those below n_sink are taken in any case
@@ -291,7 +307,7 @@ SparsePlan sparse_plan(const dcut_paged_cfg *c, int n_sel) {
   SparsePlan p = {};
   const size_t rows = c->max_rows, tg = rows * c->n_kv;
   p.max_pages = (c->max_ctx + c->page - 1) / c->page;
-  p.split = paged_split((long long)rows * c->n_kv, 1024, false);
+  p.split = paged_split((long long)rows * c->n_kv, 768, false);
   const long long most = (long long)n_sel * c->page;
   p.mc = split_max(p.split, (int)(most < c->max_ctx ? most : c->max_ctx));
   size_t off = 0;

@@ -366,6 +366,9 @@ SPARSE = {
     "one": (dict(n_q=4, n_kv=1, hd=128, page=64, d=[2, 1], ctx=[200, 63]), (1, 0, 1)),
     # more pages than a workgroup has threads
     "many": (dict(n_q=4, n_kv=2, hd=64, page=16, d=[1, 2], ctx=[9000, 4200]), (40, 2, 3)),
+    # more pages than one workgroup scores by itself, and than its threads keep in registers
+    "long": (dict(n_q=2, n_kv=1, hd=64, page=16, d=[2, 1], ctx=[20000, 16600]), (24, 1, 2)),
+    "longer": (dict(n_q=1, n_kv=1, hd=128, page=16, d=[1, 1], ctx=[70000, 900]), (100, 2, 1)),
     # more pages chosen than there are
     "all": (dict(n_q=8, n_kv=1, hd=64, page=16, d=[2, 1], ctx=[300, 20]), (64, 1, 1)),
     "group64": (dict(n_q=64, n_kv=1, hd=64, page=16, d=[1, 2], ctx=[200, 90]), (6, 1, 1)),
