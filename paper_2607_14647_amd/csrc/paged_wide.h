@@ -211,7 +211,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
     if (BEHIND) products(FirstHalf{}, vs, pf[0], pf[1]);
     weights(0);
     if (BEHIND) products(SecondHalf{}, vs, pf[2], pf[3]);
-    ld.ask(a, it, st + 2);      // here no LDS read waits for it
+    if (BEHIND) ld.ask(a, it, st + 2);      // here no LDS read waits for it
     weights(1);
 #pragma unroll
     for (int u = 0; u < 2 * KB; ++u) pf[u] = pn[u];
@@ -226,15 +226,26 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
   int special_from = it.kend;                                       // first stage with an infinite or NaN value there
 
   const int nst = (it.kend - it.kstart + KS - 1) / KS;
+  // K tiles 0 and 1 and V tile 0 are asked for at once; then interval st finds K tile st and V
+  // tile st-1 there and asks for V tile st and K tile st+1.
   ld.ask(a, it, 0);
   ld.load_k(a, it, 0, ring);
+  ld.load_v(ring + 2 * TILEB);
   ld.ask(a, it, 1);
-  // Interval st: stage st's K tile and stage st-1's V tile are there; V tile st and K tile st+1 are asked for.
+  if (nst > 1) ld.load_k(a, it, 1, ring + TILEB);
+  ld.ask(a, it, 2);
+  constexpr int LPK = Loader::LPK;
+  static_assert(2 * LPK < 16, "low bits of the wait count");
+  constexpr int WAIT_ALL = 0 | (7 << 4) | (15 << 8), WAIT_K0 = (2 * LPK) | (7 << 4) | (15 << 8), WAIT_K0_ONLY = LPK | (7 << 4) | (15 << 8);
   auto interval = [&](int st) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));            // vmcnt(0): the loads of the last interval
+    if (st == 0 && nst > 1) __builtin_amdgcn_s_waitcnt(WAIT_K0);
+    else if (st == 0) __builtin_amdgcn_s_waitcnt(WAIT_K0_ONLY);
+    else __builtin_amdgcn_s_waitcnt(WAIT_ALL);
     ring_barrier();
-    if (st < nst) ld.load_v(ring + (2 + (st & 1)) * TILEB);
-    if (st + 1 < nst) ld.load_k(a, it, st + 1, ring + ((st + 1) & 1) * TILEB);
+    if (st > 0) {
+      if (st < nst) ld.load_v(ring + (2 + (st & 1)) * TILEB);
+      if (st + 1 < nst) ld.load_k(a, it, st + 1, ring + ((st + 1) & 1) * TILEB);
+    }
     const int p0 = it.kstart + (st - 1) * KS;
     if (uniform_if(st > 0 && p0 + KS > mixed_from))                  // over the workgroup
       if (clear_specials<TILEB, NW * 64>(ring + (2 + ((st - 1) & 1)) * TILEB)) special_from = min(special_from, p0);
@@ -257,7 +268,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
   }
   for (; st <= nst; ++st) {
     interval(st);
-    ld.ask(a, it, st + 2);
+    if (st > 0) ld.ask(a, it, st + 2);
   }
   if (special_from < it.kend) {
     for (int p = max(special_from, it.klo); p < it.kend; ++p) {
