@@ -250,6 +250,23 @@ def test_scores_past_two_to_the_31():
     assert (np.abs(o - ref["out"]) <= 2.0 ** -7 * np.abs(ref["out"]) + 1e-6).mean() > 0.99
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_scores_past_two_to_the_31_in_wide_tiles(hd):
+    """As above, where a tile of rows is wider, as a request's own rows and through a shared prefix."""
+    need_gpu()
+    groups = [(0, 2, 96), (2, 3, 64)]
+    b = Batch(n_q=4, n_kv=2, hd=hd, page=16, d=[50, 40, 1], ctx=[100, 300, 130], seed=11, prefix=groups)
+    b.q, b.k = b.q * 2.0 ** 22, b.k * 2.0 ** 22
+    b.dq.mul_(2.0 ** 22)
+    b.dk.mul_(2.0 ** 22)
+    for call in ("attn", "shared"):
+        out, ls = b.run(call, groups=_groups(b, groups) if call == "shared" else None)
+        ref = b.oracle()
+        o = out.double().cpu().numpy()[: b.M]
+        assert np.isfinite(o).all() and torch.isfinite(ls[: b.M]).all()
+        assert (np.abs(o - ref["out"]) <= 2.0 ** -7 * np.abs(ref["out"]) + 1e-6).mean() > 0.99
+
+
 BAD = {
     "page_minus_one": (L.DERR_PAGE, lambda b: b.dtable.__setitem__((4, 3), -1)),
     "page_past_pool": (L.DERR_PAGE, lambda b: b.dtable.__setitem__((4, 0), b.k.shape[0])),
