@@ -155,11 +155,10 @@ k_paged_plan(PagedArgs a, int units, int TM) {
       }
       ReqRows r;
       if (!paged_request(a, i, report, r) || r0 < 0 || r0 >= (long long)r.d * a.G) continue;
-      const int P = request_prefix(a, i, r.L, report);
-      const int nc = split_count(a.split, r.L - P), ch = split_chunk(a.split, r.L - P);
+      const int nc = split_count(a.split, r.L), ch = split_chunk(a.split, r.L);
       const int rows = (int)((min(r0 + TM, (long long)r.d * a.G) - 1) / a.G) + 1;
       for (int c = 0; c < nc; ++c) {
-        const int keys = c == nc - 1 ? r.L - P - c * ch + rows : ch;
+        const int keys = c == nc - 1 ? r.L - c * ch + rows : ch;
         // the top three bits below the leading one and the exponent: 8 classes an octave
         const int cls = 255 - min((int)((__float_as_uint((float)keys) - 0x3f800000u) >> 20), 255);
         emit(cls, i, (int)r0, c);

@@ -67,24 +67,45 @@ __device__ __forceinline__ int find_run(int n, int u, int *s_cnt, Start first_ti
   return __builtin_amdgcn_readfirstlane(cnt) - 1;
 }
 
-// Keys of a group's prefix (0: none).
-__device__ __forceinline__ int shared_prefix(const PagedArgs &a, int grp) {
-  const int lo = a.group_cu[grp], hi = a.group_cu[grp + 1], P = a.prefix_len[grp];
-  if (lo < 0 || hi > a.B || lo >= hi || P <= 0) return 0;
-  return P;
-}
+// The groups of requests that share a prefix, looked through by a wave: group j's first request
+// and prefix, for up to 63 groups kept in lane j, so that one round trip to memory finds a
+// request's group (a search of its own for each work item took longer than short items' work).
+struct Groups {
+  int n, cu, prefix;
+  bool few;
+  __device__ __forceinline__ Groups(const PagedArgs &a) : n(a.n_groups), few(a.n_groups < 64) {
+    const int lane = threadIdx.x & 63;
+    cu = n > 0 ? a.group_cu[min(lane, n)] : 0;
+    prefix = n > 0 ? a.prefix_len[min(lane, n - 1)] : 0;
+  }
+  __device__ __forceinline__ int first(const PagedArgs &a, int j) const {
+    return few ? __builtin_amdgcn_readlane(cu, j) : uniform_load(a.group_cu, j);
+  }
+  // Groups whose number `below(first request, group)` calls below; they are the first ones.
+  template <typename Below>
+  __device__ __forceinline__ int count(const PagedArgs &a, Below below) const {
+    const int lane = threadIdx.x & 63;
+    int c = __popcll(__ballot(lane < n && below(cu, lane)));
+    for (int j0 = 64; j0 < n; j0 += 64) {
+      const int j = j0 + lane, f = a.group_cu[min(j, n)];
+      c += __popcll(__ballot(j < n && below(f, j)));
+    }
+    return c;
+  }
+  // Keys of group j's prefix (0: none).
+  __device__ __forceinline__ int keys(const PagedArgs &a, int j) const {
+    const int lo = first(a, j), hi = first(a, j + 1);
+    const int P = few ? __builtin_amdgcn_readlane(prefix, j) : uniform_load(a.prefix_len, j);
+    if (lo < 0 || hi > a.B || lo >= hi || P <= 0) return 0;
+    return P;
+  }
+};
 // Keys that request i (context L) reads through its group: those of the last group that starts
 // at or before i, if it holds i.
-__device__ __forceinline__ int request_prefix(const PagedArgs &a, int i, int L, bool report) {
-  if (a.n_groups == 0) return 0;
-  int lo = 0, hi = a.n_groups;              // groups before lo start at or before i
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (a.group_cu[mid] <= i) lo = mid + 1;
-    else hi = mid;
-  }
-  if (lo == 0 || i >= a.group_cu[lo]) return 0;
-  const int P = shared_prefix(a, lo - 1);
+__device__ __forceinline__ int request_prefix(const PagedArgs &a, const Groups &gr, int i, int L, bool report) {
+  const int lo = gr.count(a, [&](int f, int) { return f <= i; });
+  if (lo == 0 || i >= gr.first(a, lo)) return 0;
+  const int P = gr.keys(a, lo - 1);
   if (P > L) {
     if (report && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_GROUP);
     return 0;
@@ -116,20 +137,18 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
     return true;
   }
   if (MODE == PREFIX) {
-    auto first_tile = [&](int j) {
-      const int lo = min(max(a.group_cu[j], 0), a.B);
-      return run_tile(a.cu[lo], a.G, TM, j);
-    };
-    const int grp = find_run<THREADS>(a.n_groups, u, s_cnt, first_tile);
+    const Groups gr(a);
+    auto start = [&](int f) { return a.cu[min(max(f, 0), a.B)]; };
+    const int grp = gr.count(a, [&](int f, int j) { return run_tile(start(f), a.G, TM, j) <= u; }) - 1;
     if (grp < 0) return false;
-    const int P = shared_prefix(a, grp);
+    const int P = gr.keys(a, grp);
     if (P == 0) return false;
-    const int lo = a.group_cu[grp], hi = a.group_cu[grp + 1];
-    it.t0 = a.cu[lo];
-    const int d = a.cu[hi] - it.t0;
+    const int lo = gr.first(a, grp);
+    it.t0 = uniform_load(a.cu, lo);
+    const int d = uniform_load(a.cu, gr.first(a, grp + 1)) - it.t0;
     if (it.t0 < 0 || d <= 0 || it.t0 > a.max_rows - d) return false;
     it.rows = d * a.G;
-    const long long r0 = ((long long)u - first_tile(grp)) * TM;
+    const long long r0 = ((long long)u - run_tile(it.t0, a.G, TM, grp)) * TM;
     if (r0 < 0 || r0 >= it.rows) return false;
     it.r0 = (int)r0;
     if ((long long)P > (long long)a.table_ld << a.lpage || P > a.max_ctx) return false;
@@ -145,6 +164,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
     it.first = false;
     return true;
   }
+  const Groups gr(a);
   int i = u;
   long long r0 = 0;
   if (a.plan) {
@@ -168,7 +188,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
   if (r0 < 0 || r0 >= it.rows) return false;
   it.r0 = (int)r0;
   it.tab = a.table + (size_t)i * a.table_ld;
-  const int P = request_prefix(a, i, r.L, report);
+  const int P = request_prefix(a, gr, i, r.L, report);
   const int ncp = P > 0 ? split_count(a.psplit, P) : 0;
   const int nc = split_count(a.split, r.L - P);
   if (c >= nc) return false;
