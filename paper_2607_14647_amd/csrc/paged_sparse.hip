@@ -64,9 +64,10 @@ __device__ __forceinline__ void group_sums(const PagedArgs &a, int t, int g, dou
   }
 }
 
-// Scores of pages j0 .. j1-1 of one (row, kv head), eight lanes a page: each reads an eighth of
-// its page's bounds at once and keeps its eighth of the sums in registers.  The bounds of U
-// pages a lane are asked for together: a page is 512 bytes at a random place.
+// Scores of pages j0 .. j1-1 of one (row, kv head), eight lanes a page: lane c reads 16-byte
+// chunks c, c + 8 of its page's bounds, whole lines a load, and keeps its eighth of the sums in
+// registers.  The bounds of U pages a lane are asked for together: a page is 512 bytes at a
+// random place.  Bound by those loads: without its arithmetic it takes as long.
 template <int HD, int THREADS, int U, typename Store>
 __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *table, int g, int j0, int j1,
                                             const double *s_a, const double *s_b, Store store) {
@@ -76,8 +77,9 @@ __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *
   double av[Q], bv[Q];
 #pragma unroll
   for (int d = 0; d < Q; ++d) {
-    av[d] = s_a[c * Q + d];
-    bv[d] = s_b[c * Q + d];
+    const int at = 8 * (c + 8 * (d / 8)) + d % 8;
+    av[d] = s_a[at];
+    bv[d] = s_b[at];
   }
   for (int j = j0 + (threadIdx.x >> 3); j < j1; j += U * STEP) {
     int pg[U];
@@ -86,11 +88,11 @@ __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *
     uint4 hi[U][Q / 8], lo[U][Q / 8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const size_t row = ((size_t)((unsigned)pg[u] < (unsigned)a.n_pages ? pg[u] : 0) * a.n_kv + g) * HD + c * Q;
+      const size_t row = ((size_t)((unsigned)pg[u] < (unsigned)a.n_pages ? pg[u] : 0) * a.n_kv + g) * HD + 8 * c;
 #pragma unroll
       for (int e = 0; e < Q / 8; ++e) {
-        hi[u][e] = *(const uint4 *)(s.kmax + row + 8 * e);
-        lo[u][e] = *(const uint4 *)(s.kmin + row + 8 * e);
+        hi[u][e] = *(const uint4 *)(s.kmax + row + 64 * e);
+        lo[u][e] = *(const uint4 *)(s.kmin + row + 64 * e);
       }
     }
 #pragma unroll
