@@ -323,6 +323,8 @@ SHARED = {
     "tiles": (dict(n_q=16, n_kv=2, hd=128, page=64, d=[8, 1, 16, 4, 16, 2, 9], ctx=[700, 701, 760, 1000, 700, 710, 705]),
               [(0, 3, 640), (3, 7, 700)]),
     "zero_own": (dict(n_q=4, n_kv=1, hd=128, page=16, d=[1, 1], ctx=[48, 48]), [(0, 2, 48)]),
+    # room for many more rows than there are: prefixes cut by the largest piece
+    "long": (dict(n_q=64, n_kv=8, hd=64, page=64, d=[1, 2], ctx=[4000, 3300], extra_rows=253), [(0, 1, 3999), (1, 2, 3073)]),
 }
 
 
