@@ -395,8 +395,10 @@ int dcut_accept_rs(int B, int D, int V, float temperature, uint64_t seed, const 
  * new rows of one request; max_rows those of the batch, cu[B].  One captured graph
  * serves every batch within the bounds.
  * Supported: head_dim 64 or 128; page 16, 32, 64, 128 or 256; n_q % n_kv == 0,
- * n_q / n_kv <= 64, n_q <= 1024; max_block <= max_ctx <= 2^24; max_rows <= 131072;
- * 1 <= B <= 4096.  Pools of any size (addresses are 64 bits).
+ * n_q / n_kv <= 64, n_q <= 1024; max_block <= max_ctx <= 2^24; max_rows <= 131072,
+ * max_rows n_q <= 2^26; 1 <= B <= 4096; attention of fewer than 2^24 work items, for
+ * which dcut_paged_workspace_bytes answers (decoding B n_kv = 4096 to contexts of 2^22,
+ * say).  Pools of any size (addresses are 64 bits).
  */
 typedef struct {
   int n_q, n_kv, head_dim;
@@ -452,8 +454,8 @@ int dcut_paged_append(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B,
  * block of drafts verifies, any number is a (piece of a) prompt; requests without
  * rows are skipped.  A key that a row does not see never reaches it, whatever it holds.
  * A row whose scores are all minus infinity gives 0 and a log sum of minus infinity.
- * A row's result depends on its own request and the launch bounds only: bitwise
- * the same whatever other rows and requests hold.
+ * A row's result depends on its own request and the launch's sizes (cfg, B) only:
+ * bitwise the same whatever other rows and requests hold.
  *
  *   q       dev [max_rows][n_q][head_dim] bf16, row stride ldq elements, a multiple of 8
  *   cu      dev [B+1]; ctx_len dev [B]

@@ -11,6 +11,8 @@ namespace dcut {
 constexpr int PAGED_MAX_ROWS = 1 << 17;
 constexpr int PAGED_MAX_CTX = 1 << 24;
 constexpr int PAGED_MAX_GROUP = 64;       // query heads of a kv head
+constexpr int PAGED_MAX_PAIRS = 1 << 26;  // (row, query head) pairs: eight a workgroup of the merge, a grid has fewer than 2^32 threads
+constexpr long long PAGED_MAX_ITEMS = 0xffffff;  // work items of a launch, 256 threads each, likewise
 constexpr int PLAN_HEAD = 256;
 
 // Key chunks of a row: a run of L keys is cut into pieces of chunk(L) keys, a multiple of 64,
@@ -77,8 +79,8 @@ __device__ __forceinline__ bool paged_request(const PagedArgs &a, int i, bool re
 __device__ __forceinline__ int uniform_int(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ bool uniform_if(bool x) { return uniform_int(x) != 0; }
 
-// Uniform loads from arrays that no kernel of the call writes: one scalar load instead of a
-// vector load, whose wait would drain the operand stream in flight.
+// Uniform loads from arrays that the running kernel does not write: one scalar load instead of
+// a vector load, whose wait would drain the operand stream in flight.
 typedef __attribute__((address_space(4))) const int32_t const_i32;
 __device__ __forceinline__ int uniform_load(const int32_t *p, int idx) {
   const uintptr_t b = (uintptr_t)(p + idx);

@@ -202,20 +202,17 @@ long long items(long long units, int n_kv, int mc) { return units * n_kv * mc; }
 template <int HD, int MODE>
 int launch_stream(const PagedArgs &a, int units, int mc, hipStream_t s) {
   const long long n = items(units, a.n_kv, mc);
-  if (n > 0x7fffffffLL) return DCUT_EUNSUPPORTED;
   return launch(DCUT_KERNEL_PAGED_ATTN, k_paged_stream<HD, MODE>, dim3((unsigned)n), dim3(256), stream_lds(HD), s, a, units);
 }
 template <int HD>
 int launch_own(const PagedArgs &a, int rows, int units, int mc, hipStream_t s) {
   if (rows == 64) return launch_stream<HD, OWN>(a, units, mc, s);
   const long long n = items(units, a.n_kv, mc);
-  if (n > 0x7fffffffLL) return DCUT_EUNSUPPORTED;
   return launch(DCUT_KERNEL_PAGED_ATTN, k_paged_wide<HD>, dim3((unsigned)n), dim3(256), wide_lds(HD), s, a, units);
 }
 template <int HD>
 int launch_shared(const PagedArgs &a, int rows, int pre_units, int mc_pre, int units, int mc, hipStream_t s) {
   const long long pre = items(pre_units, a.n_kv, mc_pre), n = pre + items(units, a.n_kv, mc);
-  if (n > 0x7fffffffLL) return DCUT_EUNSUPPORTED;
   const size_t lds = wide_lds(HD) > stream_lds(HD) ? wide_lds(HD) : stream_lds(HD);
   if (rows == 64)
     return launch(DCUT_KERNEL_PAGED_ATTN, k_paged_shared<HD, false>, dim3((unsigned)n), dim3(256), lds, s, a, pre_units, (int)pre, units);
@@ -236,6 +233,7 @@ int merge(const PagedArgs &a, int hd, hipStream_t s) {
 struct AttnPlan {
   Split own, pre;
   int rows, mc_own, mc_pre, units;
+  long long items;          // workgroups of the attention kernel (shared: at most)
   size_t part, row_nc, plan, plan_bytes, total;
 };
 // Items a launch may have before they are listed longest first: what fits about one round of
@@ -259,6 +257,7 @@ AttnPlan attn_plan(const dcut_paged_cfg *c, int B, bool shared) {
     p.pre.cmax = eighth > 1536 ? eighth : 1536;
     p.mc_pre = split_max(p.pre, c->max_ctx);
   }
+  p.items = items(p.units, c->n_kv, p.mc_own) + items(shared ? tile_bound(c->max_rows, G, WIDE_ROWS, B) : 0, c->n_kv, p.mc_pre);
   const int mc = p.mc_own + p.mc_pre;
   size_t off = 0;
   p.part = off;
@@ -297,6 +296,7 @@ int paged_cfg_check(const dcut_paged_cfg *c, int B) {
   if ((c->page & (c->page - 1)) || c->page < 16 || c->page > 256) return DCUT_EUNSUPPORTED;
   if (c->n_q / c->n_kv > PAGED_MAX_GROUP || c->n_q > 1024) return DCUT_EUNSUPPORTED;
   if (c->max_rows > PAGED_MAX_ROWS || c->max_ctx > PAGED_MAX_CTX) return DCUT_EUNSUPPORTED;
+  if ((long long)c->max_rows * c->n_q > PAGED_MAX_PAIRS) return DCUT_EUNSUPPORTED;
   return DCUT_OK;
 }
 int paged_pages_check(const dcut_paged_cfg *c, const dcut_pages *p) {
@@ -317,7 +317,10 @@ PagedArgs paged_args(const dcut_paged_cfg *c, const dcut_pages *p, int B, const 
   return a;
 }
 
-size_t paged_attn_ws_bytes(const dcut_paged_cfg *c, int B, bool shared) { return attn_plan(c, B, shared).total; }
+size_t paged_attn_ws_bytes(const dcut_paged_cfg *c, int B, bool shared) {
+  const AttnPlan p = attn_plan(c, B, shared);
+  return p.items > PAGED_MAX_ITEMS ? (size_t)-1 : p.total;
+}
 
 // Rows over their listed pages (a.list set, a.split, a.MC, a.part and a.row_nc too).
 int paged_list_attn_launch(const PagedArgs &a, int hd, hipStream_t s) {
@@ -345,6 +348,7 @@ extern "C" int dcut_paged_attn(const dcut_paged_cfg *cfg, const dcut_pages *page
                                int32_t *dev_err, void *ws, size_t ws_bytes, hipStream_t stream) {
   DCUT_TRY(paged_attn_check(cfg, pages, B, q, ldq, cu, ctx_len, out));
   const AttnPlan p = attn_plan(cfg, B, false);
+  if (p.items > PAGED_MAX_ITEMS) return DCUT_EUNSUPPORTED;
   if (p.total && (!ws || ws_bytes < p.total || ((uintptr_t)ws & 255))) return DCUT_EWORKSPACE;
   PagedArgs a = paged_args(cfg, pages, B, q, ldq, cu, ctx_len, out, lse, dev_err);
   a.split = p.own;
@@ -373,6 +377,7 @@ extern "C" int dcut_paged_attn_shared(const dcut_paged_cfg *cfg, const dcut_page
   if (n_groups < 1 || n_groups > B || !group_cu || !prefix_len) return DCUT_EINVAL;
   if (st != DCUT_OK) return st;
   const AttnPlan p = attn_plan(cfg, B, true);
+  if (p.items > PAGED_MAX_ITEMS) return DCUT_EUNSUPPORTED;
   if (!ws || ws_bytes < p.total || ((uintptr_t)ws & 255)) return DCUT_EWORKSPACE;
   PagedArgs a = paged_args(cfg, pages, B, q, ldq, cu, ctx_len, out, lse, dev_err);
   a.split = p.own;

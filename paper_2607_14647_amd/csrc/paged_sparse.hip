@@ -303,6 +303,7 @@ int select_launch(const SparseArgs &s, dim3 grid, hipStream_t st) {
 struct SparsePlan {
   Split split;
   int mc, max_pages;
+  long long items;            // workgroups of the attention kernel
   size_t score, list, keys, part, row_nc, total;
 };
 SparsePlan sparse_plan(const dcut_paged_cfg *c, int n_sel) {
@@ -312,6 +313,7 @@ SparsePlan sparse_plan(const dcut_paged_cfg *c, int n_sel) {
   p.split = paged_split((long long)rows * c->n_kv, 768, false);
   const long long most = (long long)n_sel * c->page;
   p.mc = split_max(p.split, (int)(most < c->max_ctx ? most : c->max_ctx));
+  p.items = (long long)tg * p.mc;
   size_t off = 0;
   p.score = off; off = align256(off + (p.max_pages > n_sel && p.max_pages > FUSED_PAGES ? tg * p.max_pages * sizeof(double) : 0));
   p.list = off; off = align256(off + tg * n_sel * sizeof(int32_t));
@@ -325,7 +327,10 @@ SparsePlan sparse_plan(const dcut_paged_cfg *c, int n_sel) {
 
 }  // namespace
 
-size_t paged_sparse_ws_bytes(const dcut_paged_cfg *c, int n_sel) { return sparse_plan(c, n_sel).total; }
+size_t paged_sparse_ws_bytes(const dcut_paged_cfg *c, int n_sel) {
+  const SparsePlan p = sparse_plan(c, n_sel);
+  return p.items > PAGED_MAX_ITEMS ? (size_t)-1 : p.total;
+}
 
 }  // namespace dcut
 
@@ -344,6 +349,7 @@ extern "C" int dcut_paged_attn_sparse(const dcut_paged_cfg *cfg, const dcut_page
   if (st != DCUT_OK) return st;
   if (n_sel > DCUT_PAGED_MAX_SEL) return DCUT_EUNSUPPORTED;
   const SparsePlan p = sparse_plan(cfg, n_sel);
+  if (p.items > PAGED_MAX_ITEMS) return DCUT_EUNSUPPORTED;
   if (!ws || ws_bytes < p.total || ((uintptr_t)ws & 255)) return DCUT_EWORKSPACE;
   SparseArgs s = {};
   s.p = paged_args(cfg, pages, B, q, ldq, cu, ctx_len, out, lse, dev_err);

@@ -24,6 +24,7 @@ KERNELS = dict(NONE=0, SELECT=1, PACK=2, NORM=3, GEMM_QKV=4, ATTN=5, ATTN_COMBIN
                PAGED_MERGE=22, PAGE_SCORE=23, PAGE_SELECT=24)
 RS_SCAN, RS_FIXED, RS_HISTORY = 0, 1, 2
 BF16, F32 = 0, 1
+_ELEMENTS = {torch.float32: F32, torch.bfloat16: BF16, torch.int16: BF16, torch.uint16: BF16}
 PAGED_CALLS = dict(attn=0, shared=1, sparse=2)
 
 EXPORTS = ["dcut_select", "dcut_verify_layer", "dcut_lm_head_argmax", "dcut_lm_head_argmax_static",
@@ -306,6 +307,8 @@ def pages_desc(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kmin: Opti
     """Descriptor of a paged cache: k, v [n_pages][n_kv][page][head_dim], table [B][columns] int32 (its rows may be
     strided), channel bounds kmin, kmax [n_pages][n_kv][head_dim] or None.  The descriptor keeps the tensors alive."""
     p = lambda t: t.data_ptr() if t is not None else None
+    if not all(t is None or t.is_contiguous() for t in (k, v, kmin, kmax)) or v.shape != k.shape or table.stride(1) != 1:
+        raise DcutError(EINVAL, "pages_desc")
     desc = Pages(p(k), p(v), p(table), k.shape[0], table.stride(0), p(kmin), p(kmax))
     desc.tensors = (k, v, table, kmin, kmax)
     return desc
@@ -324,8 +327,12 @@ def paged_append(cfg: PagedCfg, pages: Pages, B: int, cu: torch.Tensor, packed_p
                  q_out: Optional[torch.Tensor], theta: float, dev_err: Optional[torch.Tensor] = None,
                  stream=None) -> None:
     """q, k, v: [rows][...] of float32 or bf16 (also as raw 16-bit integers), rows of any stride."""
+    dtype = k.dtype
+    kind = _ELEMENTS.get(dtype)
+    if kind is None or v.dtype is not dtype or (q is not None and q.dtype is not dtype):
+        raise DcutError(EINVAL, "dcut_paged_append")
     st = _lib.dcut_paged_append(C.byref(cfg), C.byref(pages), B, _p(cu), _p(packed_pos), _p(packed_req),
-                                F32 if k.dtype == torch.float32 else BF16, _p(q), q.stride(0) if q is not None else 0,
+                                kind, _p(q), q.stride(0) if q is not None else 0,
                                 _p(k), k.stride(0), _p(v), v.stride(0), float(theta), _p(q_out), _p(dev_err),
                                 _stream(stream))
     _check(st, "dcut_paged_append")
@@ -343,6 +350,8 @@ def paged_attn(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.T
 def paged_attn_shared(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
                       out: torch.Tensor, ws: torch.Tensor, group_cu: torch.Tensor, prefix_len: torch.Tensor,
                       lse: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
+    if group_cu.numel() != prefix_len.numel() + 1:
+        raise DcutError(EINVAL, "dcut_paged_attn_shared")
     st = _lib.dcut_paged_attn_shared(C.byref(cfg), C.byref(pages), B, _p(q), q.stride(0), _p(cu), _p(ctx_len),
                                      prefix_len.numel(), _p(group_cu), _p(prefix_len), _p(out), _p(lse), _p(dev_err),
                                      _p(ws), ws.numel() * ws.element_size(), _stream(stream))

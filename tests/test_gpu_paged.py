@@ -322,6 +322,10 @@ SHARED = {
     # many rows a group: several tiles, several pieces of the prefix
     "tiles": (dict(n_q=16, n_kv=2, hd=128, page=64, d=[8, 1, 16, 4, 16, 2, 9], ctx=[700, 701, 760, 1000, 700, 710, 705]),
               [(0, 3, 640), (3, 7, 700)]),
+    # more groups than a wave has lanes, some of them empty
+    "many_groups": (dict(n_q=4, n_kv=2, hd=64, page=16, d=[1, 2] * 75, ctx=[40, 33] * 75),
+                    [(3 + 10 * i + lo, 3 + 10 * i + hi, P) for i in range(14)
+                     for lo, hi, P in ((0, 0, 5), (0, 1, 16), (1, 4, 33), (4, 6, 0), (6, 10, 17))]),
     "zero_own": (dict(n_q=4, n_kv=1, hd=128, page=16, d=[1, 1], ctx=[48, 48]), [(0, 2, 48)]),
     # room for many more rows than there are: prefixes cut by the largest piece
     "long": (dict(n_q=64, n_kv=8, hd=64, page=64, d=[1, 2], ctx=[4000, 3300], extra_rows=253), [(0, 1, 3999), (1, 2, 3073)]),

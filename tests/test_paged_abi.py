@@ -3,6 +3,7 @@ import ctypes as C
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import paged as op
 from paper_2607_14647_amd import lib as L
@@ -47,7 +48,8 @@ BAD_CFG = [(dict(n_q=0), L.EINVAL), (dict(n_q=7), L.EINVAL), (dict(n_kv=0), L.EI
            (dict(page=0), L.EINVAL), (dict(max_ctx=0), L.EINVAL), (dict(max_block=0), L.EINVAL), (dict(max_rows=0), L.EINVAL),
            (dict(max_block=1001), L.EINVAL), (dict(head_dim=96), L.EUNSUPPORTED), (dict(page=24), L.EUNSUPPORTED),
            (dict(page=8), L.EUNSUPPORTED), (dict(page=512), L.EUNSUPPORTED), (dict(n_q=130, n_kv=2), L.EUNSUPPORTED),
-           (dict(max_rows=(1 << 17) + 1), L.EUNSUPPORTED), (dict(max_ctx=(1 << 24) + 1), L.EUNSUPPORTED)]
+           (dict(max_rows=(1 << 17) + 1), L.EUNSUPPORTED), (dict(max_ctx=(1 << 24) + 1), L.EUNSUPPORTED),
+           (dict(n_q=1024, n_kv=16, head_dim=64, max_rows=(1 << 16) + 1), L.EUNSUPPORTED)]
 
 
 @pytest.mark.parametrize("kw,want", BAD_CFG)
@@ -103,6 +105,39 @@ def test_workspaces_are_checked():
     big = _cfg(max_ctx=1 << 20, max_rows=512, n_q=32, n_kv=8)
     # (132 float32 each), and a work order of one 16-byte entry per request and piece
     assert L.paged_workspace_bytes("attn", big, 512) <= 512 * 32 * 512 * 132 * 4 + 512 * 512 * 16 + 4096
+
+
+def test_launches_of_too_many_work_items_are_refused():
+    ws = C.c_void_p(0x1000)
+    many = _cfg(n_q=1024, n_kv=1024, max_ctx=1 << 24, max_rows=4096, max_block=1)
+    args = dict(q=FAKE, ldq=1 << 17, ws=ws, wsb=2 ** 63, B=4096)
+    assert _attn(many, **args) == L.EUNSUPPORTED
+    assert L.lib().dcut_paged_workspace_bytes(0, C.byref(many), 4096, 0) == 2 ** 64 - 1
+    assert L.lib().dcut_paged_workspace_bytes(1, C.byref(many), 4096, 0) == 2 ** 64 - 1
+    assert L.lib().dcut_paged_attn_shared(C.byref(many), C.byref(_pages()), 4096, FAKE, 1 << 17, FAKE, FAKE, 1, FAKE, FAKE, FAKE,
+                                          None, None, ws, 2 ** 63, None) == L.EUNSUPPORTED
+    rows = _cfg(n_q=512, n_kv=512, max_rows=1 << 17)
+    assert L.lib().dcut_paged_workspace_bytes(2, C.byref(rows), 4, 8) == 2 ** 64 - 1
+    assert L.lib().dcut_paged_attn_sparse(C.byref(rows), C.byref(_pages()), 4, FAKE, 1 << 17, FAKE, FAKE, 8, 1, 1, None, FAKE,
+                                          None, None, ws, 2 ** 63, None) == L.EUNSUPPORTED
+    decode = _cfg(n_q=4, n_kv=1, max_ctx=1 << 22, max_rows=4096, max_block=1)
+    assert L.paged_workspace_bytes("attn", decode, 4096) > 0
+
+
+def test_the_binding_refuses_what_a_pointer_cannot_say():
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    table = torch.zeros(4, 8, dtype=torch.int32)
+    L.pages_desc(k, k, table[:, :5])
+    for bad in (dict(k=k[:, :1]), dict(v=k[:2]), dict(table=table.t()), dict(kmin=k.transpose(0, 1)[0])):
+        with pytest.raises(L.DcutError):
+            L.pages_desc(**{**dict(k=k, v=k, table=table), **bad})
+    x, c = torch.zeros(4, 128), _cfg(head_dim=64)
+    pages = L.pages_desc(k, k, table)
+    for q, kk, v in ((None, x, x.bfloat16()), (x.bfloat16(), x, x), (None, x.double(), x.double())):
+        with pytest.raises(L.DcutError):
+            L.paged_append(c, pages, 4, table, table, table, q, kk, v, q, 1e4)
+    with pytest.raises(L.DcutError):
+        L.paged_attn_shared(c, pages, 4, x, table, table, x, x, table[0, :3], table[0, :3])
 
 
 def test_oracle_closed_forms():
