@@ -33,7 +33,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void *base,
   return __builtin_amdgcn_make_buffer_rsrc((void *)(((uintptr_t)hi << 32) | lo), (short)0, bytes, 0x00020000);
 }
 
-enum Mode { OWN = 0, PREFIX = 1, LIST = 2 };
+enum Mode { OWN = 0, PREFIX = 1, LIST = 2 };    // a request's own keys, a group's prefix, chosen pages
 
 // What a work item reads and computes; uniform over the workgroup.
 struct Item {
@@ -113,8 +113,8 @@ __device__ __forceinline__ int request_prefix(const PagedArgs &a, const Groups &
   return P;
 }
 
-// ALIGN: key tiles start at multiples of it.
-template <int MODE, int TM, int THREADS, int ALIGN>
+// ALIGN: key tiles start at multiples of it.  SHARED: in a call with groups.
+template <int MODE, bool SHARED, int TM, int THREADS, int ALIGN>
 __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units, int *s_cnt, Item &it) {
   it.g = idx % a.n_kv;
   const int rest = idx / a.n_kv;
@@ -164,10 +164,9 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
     it.first = false;
     return true;
   }
-  const Groups gr(a);
   int i = u;
   long long r0 = 0;
-  if (a.plan) {
+  if (!SHARED && a.plan) {
     const int e = idx / a.n_kv;
     const int4 item = ((const int4 *)((const char *)a.plan + PLAN_HEAD))[e];
     if (e >= a.plan[0]) return false;
@@ -180,7 +179,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
     if (i < 0) return false;
     r0 = ((long long)u - first_tile(i)) * TM;
   }
-  const bool report = !a.plan && c == 0 && it.g == 0 && threadIdx.x == 0;      // the plan has reported
+  const bool report = (SHARED || !a.plan) && c == 0 && it.g == 0 && threadIdx.x == 0;      // the plan has reported
   ReqRows r;
   if (!paged_request(a, i, report, r)) return false;
   it.t0 = r.t0;
@@ -188,7 +187,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
   if (r0 < 0 || r0 >= it.rows) return false;
   it.r0 = (int)r0;
   it.tab = a.table + (size_t)i * a.table_ld;
-  const int P = request_prefix(a, gr, i, r.L, report);
+  const int P = SHARED ? request_prefix(a, Groups(a), i, r.L, report) : 0;
   const int ncp = P > 0 ? split_count(a.psplit, P) : 0;
   const int nc = split_count(a.split, r.L - P);
   if (c >= nc) return false;
@@ -207,10 +206,10 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
 // The same in scalar registers: every thread found the same item, which the compiler cannot
 // see through its searches (branches of the key loop would become divergent ones: a prompt's
 // attention with 64-wide heads took 234 us instead of 178).
-template <int MODE, int TM, int THREADS, int ALIGN>
+template <int MODE, bool SHARED, int TM, int THREADS, int ALIGN>
 __device__ __forceinline__ bool make_item(const PagedArgs &a, int idx, int units, int *s_cnt, Item &it) {
   Item x;
-  if (!find_item<MODE, TM, THREADS, ALIGN>(a, idx, units, s_cnt, x)) return false;
+  if (!find_item<MODE, SHARED, TM, THREADS, ALIGN>(a, idx, units, s_cnt, x)) return false;
   it.g = uniform_int(x.g);
   it.t0 = uniform_int(x.t0);
   it.rows = uniform_int(x.rows);
@@ -258,9 +257,9 @@ __device__ __forceinline__ float row_sum(float x) {
 // tiles leave the accumulators alone.  Each row decides for itself (others multiply by 1).
 constexpr float RAISE = 8.0f;
 
-// log2(e) / sqrt(hd): scores in the exp2 domain.  A score is scaled first and the reference
-// subtracted then (no fused multiply-add): however large the scores are, the largest weight is
-// exact; scaled inside the subtraction's fma, a score past 2^31 keeps a rounding error of 2^7
+// log2(e) / sqrt(hd): scores in the exp2 domain.  Large scores are scaled first and the
+// reference subtracted then (no fused multiply-add): however large they are, the largest weight
+// is exact; scaled inside the subtraction's fma, a score past 2^34 keeps a rounding error of 2^7
 // and more, whose exp2 overflows.
 template <int HD>
 constexpr float SCORE_SCALE = 1.4426950408889634f / (HD == 128 ? 11.313708498984761f : 8.0f);

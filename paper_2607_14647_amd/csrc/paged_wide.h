@@ -175,8 +175,6 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) s[kb] *= SCORE_SCALE<HD>;
     if (uniform_if(p0 < it.klo || p0 + KS > full_end)) {    // some key of the step is hidden from some row of the wave
       const uint32_t n = (uint32_t)max(min(it.kend, kmax + 1) - it.klo, 0);      // keys from klo on that the row sees
       const int first = p0 + 4 * h - it.klo;
@@ -191,7 +189,16 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) tm[r & 3] = fmaxf(tm[r & 3], s[kb][r]);
-    const float tmax = half_max(fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3])));
+    const float smax = half_max(fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3])));
+    const float tmax = smax * SCORE_SCALE<HD>;
+    // Scaling goes into the subtraction's multiply-add (a prompt takes 2% longer otherwise)
+    // except where a score passes 2^31 (SCORE_SCALE); up to there it adds at most 2^4 to RAISE.
+    float scale = SCORE_SCALE<HD>;
+    if (__any(fabsf(smax) > 0x1p31f)) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] *= SCORE_SCALE<HD>;
+      scale = 1.0f;
+    }
     const float m_new = tmax > m_run + RAISE ? tmax : m_run;
     // a row that has seen no key yet keeps m = -inf; subtracting 0 then keeps its weights at 0
     const float sub = m_new == -__builtin_inff() ? 0.0f : m_new;
@@ -204,7 +211,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
       uint32_t *pw = (uint32_t *)&pn[2 * kb];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float pv = __builtin_amdgcn_exp2f(s[kb][r] - sub);
+        const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], scale, -sub));
         s[kb][r] = pv;
         psum[r & 3] += pv;
       }
