@@ -264,13 +264,16 @@ constexpr float RAISE = 8.0f;
 template <int HD>
 constexpr float SCORE_SCALE = 1.4426950408889634f / (HD == 128 ? 11.313708498984761f : 8.0f);
 
-// LDS layout of a tile: key r at r * ROWB, its 16-byte chunk c at place c ^ swizzle(r).  Sixteen
-// keys read at one column (K fragments), and the two chunks that a transposing read takes from
-// each of four keys, then lie in different banks.  Without the doubling (c ^ r) the transposing
-// reads of 32 x 32 tiles met four to a bank: conflicts were 60% of the LDS's cycles.
+// LDS layout of a tile: key r at r * ROWB, its 16-byte chunk c at place c ^ swizzle(r), linear in
+// r's bits.  The 16-byte places of a 256-byte line are then met once by each of
+//   - the 16 lanes that a 16-byte read serves together (0-3, 12-15 and 20-27; the others likewise),
+//     reading keys 0-15 at one chunk (32 x 32 tiles) or, in lanes 16-31, at its neighbour
+//     (16 x 16), so keys at neighbouring places are 12 apart;
+//   - the 32 lanes of a transposing read: four chunks of four keys, or two chunks of eight.
+// The conflict counter reads 0; keys at place c ^ 2 r + (r >> 3) cost a third of the LDS's cycles.
 template <int HD>
 __device__ __forceinline__ constexpr int swizzle(int r) {
-  return (HD == 128 ? (2 * r) & 14 : r & 6) | ((r >> 3) & 1);
+  return (HD == 128 ? 4 * (r & 3) : 2 * (r & 2)) | (((r >> 1) & 2) ^ (3 * ((r >> 3) & 1)));
 }
 
 // Loads of one stage of KEYS keys (a K tile and a V tile) from the pages of a work item by NW

@@ -116,7 +116,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
 
   // Fragment addresses within a stage.  K: key l32, chunk (2 s + h) ^ swizzle(key).  V: keys
   // 16 u + 8 e + 4 h + (l16 >> 2), columns 32 n + 16 g1 + 4 (l16 & 3)..+3; the column tile n
-  // flips chunk bits 2-3, e chunk bit 0.
+  // flips chunk bits 2-3, e chunk bits 0-1.
   const uint32_t ring0 = (uint32_t)(uintptr_t)(lds_void *)ring;
   const uint32_t kfrag = ring0 + l32 * ROWB + 16 * (h ^ swizzle<HD>(l32));
   const int vkey = 4 * h + (l16 >> 2);
@@ -130,7 +130,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
   auto products = [&](auto off, const uint32_t vs, const bf16x8 &p0, const bf16x8 &p1) __attribute__((always_inline)) {
     uint32_t vb[2 * NT];
 #pragma unroll
-    for (int n = 0; n < 2 * NT; ++n) vb[n] = vs ^ (64 * (n % NT)) ^ (n >= NT ? 16 : 0);
+    for (int n = 0; n < 2 * NT; ++n) vb[n] = vs ^ (64 * (n % NT)) ^ (n >= NT ? 48 : 0);
     short4v vr[4 * NT];
     read_values<decltype(off)::value>(vr, vb);
 #pragma unroll
