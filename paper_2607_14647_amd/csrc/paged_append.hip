@@ -7,6 +7,9 @@
 //
 // Bound by HBM: every element is read and written once.  A workgroup takes ROWS rows; its
 // threads first form the rows' sines and cosines in LDS, then walk the rows' 16-byte pieces.
+// 8 prompts of about 1000 rows (178 MB) 37 us with one row a workgroup, and 10 for the bounds, 3.9 TB/s
+// in all where a large copy reaches 4.8; with two and four rows a workgroup 41 and 42.
+// 64 single rows 4.4 us: a launch, two dependent loads and the sines.
 #include "paged.h"
 
 namespace dcut {
@@ -113,7 +116,7 @@ k_paged_append(AppendArgs a) {
 // Channel bounds of the pages that the appended rows filled.  A workgroup looks through 16 rows
 // (no page is smaller) for one kv head; for each that took its page's last slot it reads the
 // page's keys, 8 channels and every (256 / (HD / 8))-th key a thread, and joins the threads of
-// a channel in LDS.
+// a channel in LDS.  The keys come out of the caches that the append left them in.
 constexpr int BOUND_ROWS = 16;
 
 template <int HD>

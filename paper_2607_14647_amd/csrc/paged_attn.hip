@@ -63,7 +63,9 @@ k_paged_shared(PagedArgs a, int pre_units, int pre_items, int units) {
 
 // Merge of a (row, head)'s partials, one half wave each, in chunk order: lane c reads partial
 // c's (max, sum), so the weights of up to 32 partials cost one memory round trip, taken
-// together with the first eight partials' values.
+// together with the first eight partials' values (16 or 32 at once: 11.3 and 10.6 us for 8.0,
+// verification of batch 64).  Bound by that round trip and the launch: 4 to 5 us for a few partials
+// a row, 8 to 10 for the largest calls.
 template <int HD>
 __global__ void __launch_bounds__(256)
 k_paged_merge(PagedArgs a) {
@@ -127,7 +129,8 @@ k_paged_merge(PagedArgs a) {
 
 // The work order of the requests' own items, {request, first pair of the tile, chunk} by
 // descending number of keys (to an eighth of an octave), built by one workgroup: a count of
-// the items of each length, their places, the items.
+// the items of each length, their places, the items.  4.7 us, and verification of batch 64 takes
+// 147 us with it, 172 without.
 __global__ void __launch_bounds__(1024)
 k_paged_plan(PagedArgs a, int units, int TM) {
   extern __shared__ int s_first[];          // first tile of each request
@@ -227,9 +230,10 @@ int merge(const PagedArgs &a, int hd, hipStream_t s) {
 
 // Work items aimed at: the requests' own rows in 64-pair tiles 1536, twice the workgroup slots,
 // since their lengths differ; beside prefixes, which fill the slots first, 768; wide tiles 256.
-// Verification under three prompts of 2000 to 6000 keys: 71.2 us; own items for 1536, 74.8;
-// prefix pieces of 1024 keys, 76.6, uncapped, 76.9 (at most 3000 keys: the longest of few long
-// items ends last); own items dispatched before the prefixes 88.7, in turns with them 80.2.
+// Verification under three prompts of 2000 to 6000 keys, the mean of five batches: 83.0 us; own
+// items for 1536 and prefix pieces uncapped (two of up to 3000 keys: the longest of few long
+// items ends last), 87.0; pieces of 1024 keys 87.6.  One of the batches takes 71.2 us, own
+// items dispatched before the prefixes 88.7, in turns with them 80.2.
 struct AttnPlan {
   Split own, pre;
   int rows, mc_own, mc_pre, units;

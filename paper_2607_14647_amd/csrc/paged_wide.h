@@ -12,10 +12,10 @@
 //
 // What bounds it: the serial chain of a step (fragments, scores, maximum, exponentials,
 // rounding, products), two waves a SIMD filling each other's gaps: the matrix units are busy
-// 43% of the time.  Prompt of 4 x 2000 rows on contexts up to 2000 (262 GFLOP) 300 us, 870
-// TFLOP/s.  Tried: two 32-row blocks a wave (one wave a SIMD: 525 us when the others took 387),
+// 40% of the time, the LDS 20%.  Prompt of 4 x 2000 rows on contexts up to 2000 (262 GFLOP)
+// 298 us, 880 TFLOP/s (5% more or less with the clock).  Tried: two 32-row blocks a wave (one wave a SIMD: 525 us when the others took 387),
 // three waves a SIMD with 32-key steps (equal), 256 rows in 8 waves (equal), half of the waves
-// a phase behind (3% slower), scores and products of one step in turn (equal here, 93 us for 84
+// a phase behind (3% slower), partials written in whole rows through the LDS (equal), scores and products of one step in turn (equal here, 93 us for 84
 // where batch 64 reads 350 MB in blocks of up to 16).
 #pragma once
 #include <type_traits>
