@@ -483,7 +483,8 @@ int dcut_paged_attn(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B, c
  * be a multiple of the page; 0 shares nothing, as do requests outside every group.
  *
  *   n_groups  1 .. B;  group_cu dev [n_groups+1] non-decreasing;  prefix_len dev [n_groups]
- *   dev_err   also DCUT_DERR_GROUP where a prefix exceeds a member's ctx_len
+ *   dev_err   also DCUT_DERR_GROUP where a prefix exceeds a member's ctx_len; a fault of one
+ *             member may leave its group's rows unspecified
  *   ws        dcut_paged_workspace_bytes(1, cfg, B, 0)
  *   other arguments as for dcut_paged_attn
  */
