@@ -54,7 +54,7 @@ __device__ __forceinline__ void read_values(short4v (&r)[16], const uint32_t (&b
       "ds_read_b64_tr_b16 %15, %23 offset:%27\n\t"
       "s_waitcnt lgkmcnt(0)"
       : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]), "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
-      : "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "n"(OFF + 0), "n"(OFF + 2048), "n"(OFF + 4096), "n"(OFF + 6144)
+      : "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "n"(OFF), "n"(OFF + 2048), "n"(OFF + 2 * 2048), "n"(OFF + 3 * 2048)
       : "memory");
 }
 template <int OFF>
@@ -70,7 +70,7 @@ __device__ __forceinline__ void read_values(short4v (&r)[8], const uint32_t (&b)
       "ds_read_b64_tr_b16 %7, %11 offset:%15\n\t"
       "s_waitcnt lgkmcnt(0)"
       : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-      : "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "n"(OFF + 0), "n"(OFF + 1024), "n"(OFF + 2048), "n"(OFF + 3072)
+      : "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "n"(OFF), "n"(OFF + 1024), "n"(OFF + 2 * 1024), "n"(OFF + 3 * 1024)
       : "memory");
 }
 
