@@ -396,7 +396,7 @@ int dcut_accept_rs(int B, int D, int V, float temperature, uint64_t seed, const 
  * serves every batch within the bounds.
  * Supported: head_dim 64 or 128; page 16, 32, 64, 128 or 256; n_q % n_kv == 0,
  * n_q / n_kv <= 64, n_q <= 1024; max_block <= max_ctx <= 2^24; max_rows <= 131072,
- * max_rows n_q <= 2^26; 1 <= B <= 4096; attention of fewer than 2^24 work items, for
+ * max_rows n_q <= 2^25; 1 <= B <= 4096; attention of fewer than 2^24 work items, for
  * which dcut_paged_workspace_bytes answers (decoding B n_kv = 4096 to contexts of 2^22,
  * say).  Pools of any size (addresses are 64 bits).
  */

@@ -11,7 +11,7 @@ namespace dcut {
 constexpr int PAGED_MAX_ROWS = 1 << 17;
 constexpr int PAGED_MAX_CTX = 1 << 24;
 constexpr int PAGED_MAX_GROUP = 64;       // query heads of a kv head
-constexpr int PAGED_MAX_PAIRS = 1 << 26;  // (row, query head) pairs: eight a workgroup of the merge, a grid has fewer than 2^32 threads
+constexpr int PAGED_MAX_PAIRS = 1 << 25;  // (row, query head) pairs: four a workgroup of the merge, a grid has fewer than 2^32 threads
 constexpr long long PAGED_MAX_ITEMS = 0xffffff;  // work items of a launch, 256 threads each, likewise
 constexpr int PLAN_HEAD = 256;
 

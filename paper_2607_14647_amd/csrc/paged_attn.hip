@@ -61,45 +61,45 @@ k_paged_shared(PagedArgs a, int pre_units, int pre_items, int units) {
   }
 }
 
-// Merge of a (row, head)'s partials, one half wave each, in chunk order: lane c reads partial
-// c's (max, sum), so the weights of up to 32 partials cost one memory round trip, taken
-// together with the first eight partials' values (16 or 32 at once: 11.3 and 10.6 us for 8.0,
-// verification of batch 64).  Bound by that round trip and the launch: 4 to 5 us for a few partials
-// a row, 8 to 10 for the largest calls.
+// Merge of a (row, head)'s partials by one wave, whose halves take every second one: lane i of a
+// half reads its i-th partial's (max, sum), so the weights of up to 64 partials cost one memory
+// round trip, taken together with the first eight partials' values.  The order of the sums is fixed.
+// Bound by its round trips and the launch: 4 to 5 us for a few partials a row, 8 for 32 partials of
+// 1024 rows (by half a wave each 9.2), 8 to 10 for the largest calls (16 values at once there: 10 to 14).
 template <int HD>
 __global__ void __launch_bounds__(256)
 k_paged_merge(PagedArgs a) {
-  constexpr int PER = HD / 32, CG = 8;
-  const int lane = threadIdx.x & 31;
-  const int pair = blockIdx.x * 8 + (threadIdx.x >> 5);
+  constexpr int PER = HD / 32, CG = 4;
+  const int lane = threadIdx.x & 31, odd = (threadIdx.x >> 5) & 1;
+  const int pair = blockIdx.x * 4 + (threadIdx.x >> 6);
   const int t = pair / a.n_q;
   const int nc0 = a.row_nc[min(t, a.max_rows - 1)];
   const int M = a.cu[a.B];
   if (t >= M || t >= a.max_rows) return;
   const int nc = min(nc0, a.MC);
   if (nc <= 1) return;
-  const float *pp = a.part + (size_t)pair * a.MC * ATTN_PITCH(HD);
+  const float *pp = a.part + ((size_t)pair * a.MC + odd) * ATTN_PITCH(HD);
   float acc[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) acc[e] = 0.0f;
   float mx = -__builtin_inff(), lsum = 0.0f;
-  for (int c0 = 0; c0 < nc; c0 += 32) {
-    const int cnt = min(32, nc - c0);
+  for (int c0 = 0; c0 < nc; c0 += 64) {
+    const int both = min(64, nc - c0), cnt = (both + 1 - odd) >> 1;          // partials c0 + odd + 2 i
     const float *p0 = pp + (size_t)c0 * ATTN_PITCH(HD);
     float xv[CG][PER];
     auto load = [&](int cc) {
 #pragma unroll
       for (int u = 0; u < CG; ++u)
 #pragma unroll
-        for (int e = 0; e < PER; ++e) xv[u][e] = cc + u < cnt ? p0[(cc + u) * ATTN_PITCH(HD) + lane * PER + e] : 0.0f;
+        for (int e = 0; e < PER; ++e) xv[u][e] = cc + u < cnt ? p0[(cc + u) * 2 * ATTN_PITCH(HD) + lane * PER + e] : 0.0f;
     };
     load(0);
-    const float mv = lane < cnt ? p0[lane * ATTN_PITCH(HD) + HD] : -__builtin_inff();
-    const float lv = lane < cnt ? p0[lane * ATTN_PITCH(HD) + HD + 1] : 0.0f;
+    const float mv = lane < cnt ? p0[lane * 2 * ATTN_PITCH(HD) + HD] : -__builtin_inff();
+    const float lv = lane < cnt ? p0[lane * 2 * ATTN_PITCH(HD) + HD + 1] : 0.0f;
     float gm = mv;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) gm = fmaxf(gm, __shfl_xor(gm, off, 32));
-    const float mn = fmaxf(mx, gm), sub = mn == -__builtin_inff() ? 0.0f : mn;
+    const float mn = fmaxf(mx, half_max(gm)), sub = mn == -__builtin_inff() ? 0.0f : mn;
     const float w = __builtin_amdgcn_exp2f(mv - sub);         // 0 for an empty partial
     float ls = lane < cnt ? lv * w : 0.0f;
 #pragma unroll
@@ -116,10 +116,14 @@ k_paged_merge(PagedArgs a) {
 #pragma unroll
         for (int e = 0; e < PER; ++e) acc[e] += cc + u < cnt ? xv[u][e] * wc : 0.0f;
       }
-      if (cc + CG >= cnt) break;
+      if (2 * (cc + CG) >= both) break;
       load(cc + CG);
     }
   }
+  lsum = half_sum(lsum);
+#pragma unroll
+  for (int e = 0; e < PER; ++e) acc[e] = half_sum(acc[e]);
+  if (odd) return;
   const float inv = lsum > 0.0f ? 1.0f / lsum : lsum == 0.0f ? 0.0f : lsum;
   uint16_t *op = a.out + (size_t)pair * HD + lane * PER;
 #pragma unroll
@@ -223,7 +227,7 @@ int launch_shared(const PagedArgs &a, int rows, int pre_units, int mc_pre, int u
 }
 int merge(const PagedArgs &a, int hd, hipStream_t s) {
   if (a.MC == 1) return DCUT_OK;
-  const dim3 grid((unsigned)(((long long)a.max_rows * a.n_q + 7) / 8));
+  const dim3 grid((unsigned)(((long long)a.max_rows * a.n_q + 3) / 4));
   if (hd == 128) return launch(DCUT_KERNEL_PAGED_MERGE, k_paged_merge<128>, grid, dim3(256), 0, s, a);
   return launch(DCUT_KERNEL_PAGED_MERGE, k_paged_merge<64>, grid, dim3(256), 0, s, a);
 }

@@ -116,7 +116,7 @@ def test_launches_of_too_many_work_items_are_refused():
     assert L.lib().dcut_paged_workspace_bytes(1, C.byref(many), 4096, 0) == 2 ** 64 - 1
     assert L.lib().dcut_paged_attn_shared(C.byref(many), C.byref(_pages()), 4096, FAKE, 1 << 17, FAKE, FAKE, 1, FAKE, FAKE, FAKE,
                                           None, None, ws, 2 ** 63, None) == L.EUNSUPPORTED
-    rows = _cfg(n_q=512, n_kv=512, max_rows=1 << 17)
+    rows = _cfg(n_q=512, n_kv=512, max_rows=1 << 16)
     assert L.lib().dcut_paged_workspace_bytes(2, C.byref(rows), 4, 8) == 2 ** 64 - 1
     assert L.lib().dcut_paged_attn_sparse(C.byref(rows), C.byref(_pages()), 4, FAKE, 1 << 17, FAKE, FAKE, 8, 1, 1, None, FAKE,
                                           None, None, ws, 2 ** 63, None) == L.EUNSUPPORTED
