@@ -7,6 +7,10 @@
 // The score decides which pages are read, so it is formed in 64 bits: products of a bf16
 // value and a short sum are exact there, and two pages change places only where their
 // scores are equal to about 1 in 2^50.
+//
+// Measured: one request of 32000 keys (500 pages) 24 us, of which selection 13, attention 8 and the
+// merge 5 (with their launches); batch 16 at 16 to 64 thousand keys 56 us: selection 24 (30 MB of
+// bounds in 256-byte pieces, 15 of them reading those), the chosen pages 31, 134 MB at 4.4 TB/s.
 #include "paged.h"
 
 namespace dcut {
@@ -143,7 +147,10 @@ __device__ __forceinline__ unsigned long long order_key(double x) {
   return (u >> 63) ? ~u : u | 0x8000000000000000ull;
 }
 
-constexpr int FUSED_PAGES = 1024;     // pages up to which one workgroup scores and selects
+// Pages up to which one workgroup scores and selects: one launch less (500 pages 13.7 us, in two
+// launches 16.7; batch 16 of up to 1000 pages 24.4 and 25.3).  Past it the scores of one (row, kv
+// head) are worth several workgroups.
+constexpr int FUSED_PAGES = 1024;
 
 // The n_sel pages of one (row, kv head): the first n_sink and the last n_local, then by score,
 // ties to the lower page.  Each thread owns a run of pages.  A radix select over the scores'
@@ -310,7 +317,7 @@ SparsePlan sparse_plan(const dcut_paged_cfg *c, int n_sel) {
   SparsePlan p = {};
   const size_t rows = c->max_rows, tg = rows * c->n_kv;
   p.max_pages = (c->max_ctx + c->page - 1) / c->page;
-  p.split = paged_split((long long)rows * c->n_kv, 768, false);
+  p.split = paged_split((long long)rows * c->n_kv, 768, false);     // one round of three workgroups a CU
   const long long most = (long long)n_sel * c->page;
   p.mc = split_max(p.split, (int)(most < c->max_ctx ? most : c->max_ctx));
   p.items = (long long)tg * p.mc;
