@@ -192,12 +192,15 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, const Item &it, un
     const float smax = half_max(fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3])));
     const float tmax = smax * SCORE_SCALE<HD>;
     // Scaling goes into the subtraction's multiply-add (a prompt takes 2% longer otherwise)
-    // except where a score passes 2^31 (SCORE_SCALE); up to there it adds at most 2^4 to RAISE.
+    // except for a row whose score passes 2^31 (SCORE_SCALE); up to there it adds at most 2^4 to
+    // RAISE.  Each row decides from its own scores: the others multiply by 1.
+    const bool big = fabsf(smax) > 0x1p31f && smax != -__builtin_inff();
     float scale = SCORE_SCALE<HD>;
-    if (__any(fabsf(smax) > 0x1p31f)) {
+    if (__any(big)) {
+      const float first = big ? SCORE_SCALE<HD> : 1.0f;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) s[kb] *= SCORE_SCALE<HD>;
-      scale = 1.0f;
+      for (int kb = 0; kb < KB; ++kb) s[kb] *= first;
+      scale = big ? 1.0f : SCORE_SCALE<HD>;
     }
     const float m_new = tmax > m_run + RAISE ? tmax : m_run;
     // a row that has seen no key yet keeps m = -inf; subtracting 0 then keeps its weights at 0

@@ -752,3 +752,66 @@ def test_selected_rows_of_the_step(cid):
     torch.cuda.synchronize()
     b.q, b.k, b.v = (x.double().cpu().numpy() for x in (q_out, b.dk, b.dv))
     b.check(out, ls, b.oracle(), what=c.name)
+
+
+def _keep(b, d2):
+    """The batch with only the first d2[i] new rows of each request kept: queries packed again, cu, old and new row
+    numbers."""
+    cu2 = np.concatenate([[0], np.cumsum(d2)]).astype(np.int32)
+    old = np.concatenate([np.arange(b.cu[i], b.cu[i] + d2[i]) for i in range(b.B)])
+    q2 = b.dq.clone()
+    q2[: len(old)] = b.dq[torch.from_numpy(old).cuda()]
+    b.dq = q2
+    b.dcu.copy_(torch.from_numpy(cu2))
+    return torch.from_numpy(old).cuda(), torch.arange(len(old), device="cuda")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_q,kept", [(2, 100), (2, 70), (2, 130), (8, 41), (8, 30)])
+def test_wide_rows_do_not_depend_on_the_rows_kept(hd, n_q, kept):
+    """160 rows a request against fewer: waves partly filled, and steps of keys that only the request's later rows see.
+    The rows that stay are bitwise what they were."""
+    need_gpu()
+    ctx = [90, 0, 31, 64, 104, 127]
+    b = Batch(n_q=n_q, n_kv=2, hd=hd, page=16, d=[160] * len(ctx), ctx=ctx, seed=31)
+    cfg = b.cfg()
+    out, ls = b.run(cfg=cfg)
+    old, new = _keep(b, [kept] * b.B)
+    out2, ls2 = b.run(cfg=cfg)
+    torch.cuda.synchronize()
+    assert torch.equal(out[old], out2[new]) and torch.equal(ls[old], ls2[new])
+
+
+@pytest.mark.parametrize("value", [np.inf, -np.inf, 2.0 ** 60])
+@pytest.mark.parametrize("name", ["wide", "prompt", "prompt64", "verify"])
+def test_one_channel_of_a_later_key_never_reaches_earlier_rows(name, value):
+    """One channel of the last row's key is infinite or far above the others, so that its scores are, not NaN: earlier
+    rows are bitwise what they were."""
+    need_gpu()
+    b = Batch(seed=32, **ATTN[name])
+    out, ls = b.run()
+    rows = []
+    for i in range(b.B):
+        if b.d[i]:
+            p = int(b.ctx[i] + b.d[i] - 1)
+            b.dk[int(b.table[i, p // b.page]), :, p % b.page, 5] = value
+            rows += list(range(b.cu[i], b.cu[i + 1] - 1))
+    got, gls = b.run()
+    torch.cuda.synchronize()
+    rows = torch.tensor(rows, device="cuda")
+    assert torch.equal(out[rows], got[rows]) and torch.equal(ls[rows], gls[rows])
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_shared_rows_do_not_depend_on_a_members_queries(hd):
+    """One member's queries are scaled by 2^34 (its scores pass 2^31): the others' rows are bitwise what they were."""
+    need_gpu()
+    groups = [(0, 4, 200)]
+    b = Batch(n_q=4, n_kv=2, hd=hd, page=16, d=[3, 40, 1, 5], ctx=[210, 240, 200, 330], seed=33, prefix=groups)
+    g = _groups(b, groups)
+    out, ls = b.run("shared", groups=g)
+    b.dq[b.cu[2]: b.cu[3]] *= 2.0 ** 34
+    got, gls = b.run("shared", groups=g)
+    torch.cuda.synchronize()
+    others = torch.tensor([t for t in range(b.M) if not b.cu[2] <= t < b.cu[3]], device="cuda")
+    assert torch.equal(out[others], got[others]) and torch.equal(ls[others], gls[others])
