@@ -23,7 +23,7 @@ k_paged_stream(PagedArgs a, int units) {
   extern __shared__ __align__(1024) unsigned char ring[];
   __shared__ int s_cnt[STREAM_WAVES];
   Item it;
-  if (!make_item<MODE, false, 16 * STREAM_WAVES, 64 * STREAM_WAVES, STREAM_KEYS>(a, blockIdx.x, units, s_cnt, it)) return;
+  if (!make_item<MODE, false, 16 * STREAM_WAVES, 64 * STREAM_WAVES>(a, blockIdx.x, units, s_cnt, it)) return;
   stream_body<HD, MODE>(a, it, ring);
 }
 
@@ -33,7 +33,7 @@ k_paged_wide(PagedArgs a, int units) {
   extern __shared__ __align__(1024) unsigned char ring[];
   __shared__ int s_cnt[WIDE_WAVES];
   Item it;
-  if (!make_item<OWN, false, WIDE_ROWS, 64 * WIDE_WAVES, WIDE_KEYS>(a, blockIdx.x, units, s_cnt, it)) return;
+  if (!make_item<OWN, false, WIDE_ROWS, 64 * WIDE_WAVES>(a, blockIdx.x, units, s_cnt, it)) return;
   wide_body<HD, OWN>(a, it, ring);
 }
 
@@ -47,16 +47,16 @@ k_paged_shared(PagedArgs a, int pre_units, int pre_items, int units) {
   __shared__ int s_cnt[4];
   Item it;
   if ((int)blockIdx.x < pre_items) {
-    if (!make_item<PREFIX, true, WIDE_ROWS, 256, WIDE_KEYS>(a, blockIdx.x, pre_units, s_cnt, it)) return;
+    if (!make_item<PREFIX, true, WIDE_ROWS, 256>(a, blockIdx.x, pre_units, s_cnt, it)) return;
     wide_body<HD, PREFIX>(a, it, ring);
     return;
   }
   const int idx = blockIdx.x - pre_items;
   if (WIDE) {
-    if (!make_item<OWN, true, WIDE_ROWS, 256, WIDE_KEYS>(a, idx, units, s_cnt, it)) return;
+    if (!make_item<OWN, true, WIDE_ROWS, 256>(a, idx, units, s_cnt, it)) return;
     wide_body<HD, OWN>(a, it, ring);
   } else {
-    if (!make_item<OWN, true, 64, 256, STREAM_KEYS>(a, idx, units, s_cnt, it)) return;
+    if (!make_item<OWN, true, 64, 256>(a, idx, units, s_cnt, it)) return;
     stream_body<HD, OWN>(a, it, ring);
   }
 }

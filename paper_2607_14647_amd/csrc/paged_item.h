@@ -41,7 +41,7 @@ struct Item {
   int t0, rows, r0;    // first packed row of the unit, its (row, head) pairs, first of this tile
   const int32_t *tab;  // page of keys j*page.. of the unit
   int klo, kend;       // keys of the chunk; below klo and from kend on: none
-  int kstart;          // first key tile
+  int kstart;          // first key of the first key tile, in klo's page, a multiple of 16
   int diag;            // packed row t0 + r sees keys up to diag + r
   int nc, slot;        // partials of the rows, and which this one is
   bool first;          // this item notes the rows' count of partials
@@ -113,8 +113,8 @@ __device__ __forceinline__ int request_prefix(const PagedArgs &a, const Groups &
   return P;
 }
 
-// ALIGN: key tiles start at multiples of it.  SHARED: in a call with groups.
-template <int MODE, bool SHARED, int TM, int THREADS, int ALIGN>
+// SHARED: in a call with groups.
+template <int MODE, bool SHARED, int TM, int THREADS>
 __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units, int *s_cnt, Item &it) {
   it.g = idx % a.n_kv;
   const int rest = idx / a.n_kv;
@@ -195,7 +195,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
   const int last_row = (min(it.r0 + TM, it.rows) - 1) / a.G;
   it.klo = P + c * ch;
   it.kend = c == nc - 1 ? r.L + last_row + 1 : P + (c + 1) * ch;
-  it.kstart = it.klo & ~(ALIGN - 1);
+  it.kstart = it.klo & ~15;                 // within klo's page: the table's entries before it may be unset
   it.diag = r.L;
   it.nc = ncp + nc;
   it.slot = ncp + c;
@@ -206,10 +206,10 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
 // The same in scalar registers: every thread found the same item, which the compiler cannot
 // see through its searches (branches of the key loop would become divergent ones: a prompt's
 // attention with 64-wide heads took 234 us instead of 178).
-template <int MODE, bool SHARED, int TM, int THREADS, int ALIGN>
+template <int MODE, bool SHARED, int TM, int THREADS>
 __device__ __forceinline__ bool make_item(const PagedArgs &a, int idx, int units, int *s_cnt, Item &it) {
   Item x;
-  if (!find_item<MODE, SHARED, TM, THREADS, ALIGN>(a, idx, units, s_cnt, x)) return false;
+  if (!find_item<MODE, SHARED, TM, THREADS>(a, idx, units, s_cnt, x)) return false;
   it.g = uniform_int(x.g);
   it.t0 = uniform_int(x.t0);
   it.rows = uniform_int(x.rows);

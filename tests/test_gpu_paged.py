@@ -815,3 +815,17 @@ def test_shared_rows_do_not_depend_on_a_members_queries(hd):
     torch.cuda.synchronize()
     others = torch.tensor([t for t in range(b.M) if not b.cu[2] <= t < b.cu[3]], device="cuda")
     assert torch.equal(out[others], got[others]) and torch.equal(ls[others], gls[others])
+
+
+@pytest.mark.parametrize("page,P,d", [(16, 16, 1), (16, 48, 1), (16, 50, 2), (16, 16, 40), (16, 48, 40), (32, 32, 40), (32, 96, 17)])
+def test_shared_reads_prefixes_through_the_first_member_only(page, P, d):
+    """The prefix's columns of the other members' tables are unset: right rows and no fault, whatever the prefix's place
+    within a step of keys."""
+    need_gpu()
+    groups = [(0, 3, P)]
+    b = Batch(n_q=8, n_kv=2, hd=64, page=page, d=[1, d, 2], ctx=[P + 5, P, P + 70], seed=34, prefix=groups)
+    ref = b.oracle()
+    b.dtable[1:, : P // page] = -1
+    out, ls = b.run("shared", groups=_groups(b, groups))
+    b.check(out, ls, ref, what=f"page {page} prefix {P}")
+    assert int(b.err.item()) == 0
