@@ -436,7 +436,8 @@ enum { DCUT_PAGED_MAX_SEL = 4096 };       /* pages dcut_paged_attn_sparse may re
  *   q_out   dev [max_rows][n_q][head_dim] bf16 out (must not overlap the inputs)
  *   dev_err DCUT_DERR_CAPACITY for a row whose request is outside [0, B) or whose
  *           position lies outside the table or max_ctx, DCUT_DERR_PAGE for a bad page:
- *           the row is not appended
+ *           the row is not appended; DCUT_DERR_CAPACITY too if cu[B] < 0 or > max_rows,
+ *           then rows from max_rows on are not appended
  * Rows from cu[B] on are neither read nor written.
  * Returns DCUT_OK, DCUT_EINVAL, DCUT_EUNSUPPORTED, DCUT_EHIP.
  */

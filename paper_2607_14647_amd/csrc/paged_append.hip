@@ -50,8 +50,11 @@ k_paged_append(AppendArgs a) {
   __shared__ long long s_slot[ROWS];        // element offset of (row's page, kv head 0, slot), or -1
   const int tid = threadIdx.x;
   const int r0 = blockIdx.x * ROWS;
-  const int M = min(a.cu[a.B], a.max_rows);
-  if (r0 >= M) return;
+  const int end = a.cu[a.B], M = min(end, a.max_rows);
+  if (r0 >= M) {
+    if (end < 0 && tid == 0 && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
+    return;
+  }
   const int page = 1 << a.lpage;
   for (int e = tid; e < ROWS * HALF; e += 256) {
     const int r = e / HALF, j = e - r * HALF;
@@ -65,6 +68,7 @@ k_paged_append(AppendArgs a) {
     long long slot = -1;
     if (r0 + tid < M) {
       const int i = a.req[r0 + tid], p = a.pos[r0 + tid];
+      if (end > a.max_rows && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
       if (i < 0 || i >= a.B || p < 0 || p >= a.max_ctx || (p >> a.lpage) >= a.table_ld) {
         if (a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
       } else {

@@ -829,3 +829,23 @@ def test_shared_reads_prefixes_through_the_first_member_only(page, P, d):
     out, ls = b.run("shared", groups=_groups(b, groups))
     b.check(out, ls, ref, what=f"page {page} prefix {P}")
     assert int(b.err.item()) == 0
+
+
+@pytest.mark.parametrize("end", [9, 2 ** 31 - 1, -3])
+def test_append_row_counts_outside_the_bounds(end):
+    """cu[B] above max_rows, or negative: its bit; the rows up to max_rows are appended, no others are touched."""
+    need_gpu()
+    b = Batch(n_q=4, n_kv=2, hd=64, page=16, d=[1] * 9, ctx=[3, 20, 40, 15, 31, 7, 0, 16, 2], seed=35)
+    b.bounds()
+    q, k, v, pos, req, *_ = _append_case(b, torch.bfloat16, 36)
+    k0 = b.dk.clone()
+    q_out = torch.full((b.rows, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    b.dcu[b.B] = end
+    L.paged_append(b.cfg(max_rows=6), b.pages(), b.B, b.dcu, dev(pos, torch.int32), dev(req, torch.int32), q, k, v, q_out, THETA,
+                   dev_err=b.err)
+    torch.cuda.synchronize()
+    live = 6 if end > 0 else 0
+    assert int(b.err.item()) == L.DERR_CAPACITY
+    assert (q_out[live:] == 7.0).all() and (q_out[:live] != 7.0).any(-1).all()
+    changed = (b.dk != k0).flatten(1).any(1).nonzero().flatten().tolist()
+    assert sorted(changed) == sorted(int(b.table[i, b.ctx[i] // 16]) for i in range(live))
