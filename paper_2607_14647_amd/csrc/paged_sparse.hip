@@ -28,6 +28,7 @@ struct SparseArgs {
 
 // A row's request and where it sits, found by all threads: the one that holds the request's
 // bounds passes them on.  False (for all) where the row is not live or its request is refused.
+// With `report` every request's faults are noted, that of one without live rows too.
 struct RowAt {
   int i, pos;
 };
@@ -37,9 +38,10 @@ __device__ __forceinline__ bool find_row(const PagedArgs &a, int t, int *s_row, 
   __syncthreads();
   for (int j = threadIdx.x; j < a.B; j += THREADS) {
     const int lo = a.cu[j], hi = a.cu[j + 1], L = a.ctx_len[j];
+    ReqRows r;
+    if (report) paged_request(a, j, true, r);
     if (lo <= t && t < hi) {
-      ReqRows r;
-      if (t < a.max_rows && t < a.cu[a.B] && paged_request(a, j, report, r)) {
+      if (t < a.max_rows && t < a.cu[a.B] && paged_request(a, j, false, r)) {
         s_row[1] = L + t - lo;
         s_row[0] = j;
       }
@@ -169,7 +171,7 @@ k_page_select(SparseArgs s) {
   const int t = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
   const size_t tg = (size_t)t * a.n_kv + g;
   RowAt row;
-  if (!find_row<ST>(a, t, s_row, g == 0, row)) {
+  if (!find_row<ST>(a, t, s_row, t == 0 && g == 0, row)) {
     if (tid == 0) s.list_keys[tg] = 0;
     return;
   }

@@ -849,3 +849,27 @@ def test_append_row_counts_outside_the_bounds(end):
     assert (q_out[live:] == 7.0).all() and (q_out[:live] != 7.0).any(-1).all()
     changed = (b.dk != k0).flatten(1).any(1).nonzero().flatten().tolist()
     assert sorted(changed) == sorted(int(b.table[i, b.ctx[i] // 16]) for i in range(live))
+
+
+def test_sparse_and_shared_bad_row_counts():
+    """Requests whose rows lie past max_rows, or that end before they start: their bit, other rows bitwise unchanged."""
+    need_gpu()
+    sel = (4, 1, 1)
+    for call in ("sparse", "shared"):
+        b = Batch(n_q=4, n_kv=2, hd=64, page=16, d=[6, 5], ctx=[200, 300], seed=37, prefix=[(0, 2, 160)])
+        b.bounds()
+        cfg = b.cfg(max_rows=6)
+        kw = dict(cfg=cfg, sel=sel) if call == "sparse" else dict(cfg=cfg, groups=_groups(b, [(0, 2, 160)]))
+        b.dcu.copy_(torch.tensor([0, 6, 6]))
+        want, _ = b.run(call, **kw)
+        assert int(b.err.item()) == 0
+        for cu in ([0, 6, 11], [0, 6, 2 ** 31 - 1], [0, 6, 4]):
+            b.err.zero_()
+            b.dcu.copy_(torch.tensor(cu))
+            got, _ = b.run(call, **kw)
+            torch.cuda.synchronize()
+            note(f"{call} cu {cu}: err {int(b.err.item())}")
+            assert int(b.err.item()) == L.DERR_CAPACITY
+            if call == "sparse" and cu[2] > 6:
+                assert torch.equal(want[:6], got[:6])
+            assert (got[6:] == 7.0).all()
