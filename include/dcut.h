@@ -509,6 +509,7 @@ int dcut_paged_attn_shared(const dcut_paged_cfg *cfg, const dcut_pages *pages, i
  *   blocks   dev [max_rows][n_kv][n_sel] int32 out (nullable): the table columns of the
  *            pages read, ascending, then -1
  *   pages    with kmin and kmax of every full page
+ *   dev_err  DCUT_DERR_PAGE for any bad page that a row may choose from
  *   ws       dcut_paged_workspace_bytes(2, cfg, B, n_sel)
  *   other arguments as for dcut_paged_attn
  */

@@ -73,7 +73,8 @@ __device__ __forceinline__ void group_sums(const PagedArgs &a, int t, int g, dou
 // Scores of pages j0 .. j1-1 of one (row, kv head), eight lanes a page: lane c reads 16-byte
 // chunks c, c + 8 of its page's bounds, whole lines a load, and keeps its eighth of the sums in
 // registers.  The bounds of U pages a lane are asked for together: a page is 512 bytes at a
-// random place.  Bound by those loads: without its arithmetic it takes as long.
+// random place.  Bound by those loads: without its arithmetic it takes as long.  A page number
+// outside the pool is scored with page 0's bounds and reported, chosen or not.
 template <int HD, int THREADS, int U, typename Store>
 __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *table, int g, int j0, int j1,
                                             const double *s_a, const double *s_b, Store store) {
@@ -87,6 +88,7 @@ __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *
     av[d] = s_a[at];
     bv[d] = s_b[at];
   }
+  unsigned worst = 0;
   for (int j = j0 + (threadIdx.x >> 3); j < j1; j += U * STEP) {
     int pg[U];
 #pragma unroll
@@ -94,6 +96,7 @@ __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *
     uint4 hi[U][Q / 8], lo[U][Q / 8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      worst = max(worst, (unsigned)pg[u]);
       const size_t row = ((size_t)((unsigned)pg[u] < (unsigned)a.n_pages ? pg[u] : 0) * a.n_kv + g) * HD + 8 * c;
 #pragma unroll
       for (int e = 0; e < Q / 8; ++e) {
@@ -119,6 +122,7 @@ __device__ __forceinline__ void score_pages(const SparseArgs &s, const int32_t *
       if (c == 0 && j + u * STEP < j1) store(j + u * STEP, acc);
     }
   }
+  if (worst >= (unsigned)a.n_pages && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_PAGE);
 }
 
 constexpr int SCORE_PAGES = 256;      // pages a workgroup of k_page_score takes

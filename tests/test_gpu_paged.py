@@ -873,3 +873,34 @@ def test_sparse_and_shared_bad_row_counts():
             if call == "sparse" and cu[2] > 6:
                 assert torch.equal(want[:6], got[:6])
             assert (got[6:] == 7.0).all()
+
+
+@pytest.mark.parametrize("shape,sel", [(dict(n_q=8, n_kv=2, hd=128, page=16, d=[1, 2], ctx=[1500, 700]), (8, 1, 2)),
+                                       (dict(n_q=2, n_kv=1, hd=64, page=16, d=[1, 1], ctx=[300, 20000]), (8, 1, 2))])
+@pytest.mark.parametrize("entry", [-1, 2 ** 30])
+def test_sparse_reports_pages_that_are_not_chosen(shape, sel, entry):
+    """A bad table entry among the pages that a row may choose from: its bit, wherever its score would have put it."""
+    need_gpu()
+    b = Batch(seed=38, **shape)
+    b.bounds()
+    blocks = torch.zeros(b.rows, b.n_kv, sel[0], dtype=torch.int32, device="cuda")
+    want, _ = b.run("sparse", sel=sel, blocks=blocks)
+    assert int(b.err.item()) == 0
+    i = b.B - 1
+    last = b.M - 1
+    rows = list(range(b.cu[i], b.cu[i + 1]))
+    chosen = set(blocks[rows].flatten().tolist())
+    page0 = int((b.dtable[i] == 0).nonzero()) if bool((b.dtable[i] == 0).any()) else -1
+    free = [j for j in range(2, int(b.ctx[i]) // b.page - 2) if j not in chosen and j != page0]
+    for j in (free[0], free[len(free) // 2], free[-1]):
+        b.err.zero_()
+        good = int(b.dtable[i, j])
+        # the entry takes the place of a page whose bounds nobody prefers
+        b.dtable[i, j] = entry
+        b.dkmin[0], b.dkmax[0] = 0.0, -1e30
+        got, _ = b.run("sparse", sel=sel)
+        torch.cuda.synchronize()
+        assert int(b.err.item()) == L.DERR_PAGE, j
+        others = torch.tensor([t for t in range(b.M) if t not in rows], device="cuda")
+        assert torch.isfinite(got[others].float()).all()
+        b.dtable[i, j] = good
