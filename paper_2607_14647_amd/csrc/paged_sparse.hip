@@ -53,7 +53,8 @@ __device__ __forceinline__ bool find_row(const PagedArgs &a, int t, int *s_row, 
   return row.i >= 0;
 }
 
-// The group's sums of one (row, kv head), by the first HD threads of the workgroup.
+// The group's sums of one (row, kv head), by the first HD threads of the workgroup.  A NaN stays
+// one, in both sums, and so in every score.
 template <int HD>
 __device__ __forceinline__ void group_sums(const PagedArgs &a, int t, int g, double *s_a, double *s_b) {
   if (threadIdx.x < HD) {
@@ -62,8 +63,8 @@ __device__ __forceinline__ void group_sums(const PagedArgs &a, int t, int g, dou
 #pragma unroll 4
     for (int h = 0; h < a.G; ++h) {
       const float x = bf2f(q[h * HD]);
-      p += (double)fmaxf(x, 0.0f);
-      n += (double)fminf(x, 0.0f);
+      p += (double)(x < 0.0f ? 0.0f : x);
+      n += (double)(x > 0.0f ? 0.0f : x);
     }
     s_a[threadIdx.x] = p;
     s_b[threadIdx.x] = n;

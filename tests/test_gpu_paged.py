@@ -904,3 +904,23 @@ def test_sparse_reports_pages_that_are_not_chosen(shape, sel, entry):
         others = torch.tensor([t for t in range(b.M) if t not in rows], device="cuda")
         assert torch.isfinite(got[others].float()).all()
         b.dtable[i, j] = good
+
+
+def test_sparse_nan_queries():
+    """A NaN in a query makes every score of its row and kv head NaN: all pages tie, the lowest are read.  Other rows and
+    kv heads choose as before."""
+    need_gpu()
+    for shape, sel in ((dict(n_q=8, n_kv=2, hd=128, page=16, d=[1, 2], ctx=[1500, 700]), (8, 1, 2)),
+                       (dict(n_q=4, n_kv=2, hd=64, page=16, d=[1], ctx=[20000]), (8, 0, 1))):
+        b = Batch(seed=39, **shape)
+        b.bounds()
+        b.q[0, 1, 7] = np.nan
+        b.dq[0, b.hd + 7] = float("nan")
+        blocks = torch.zeros(b.rows, b.n_kv, sel[0], dtype=torch.int32, device="cuda")
+        out, _ = b.run("sparse", sel=sel, blocks=blocks)
+        want = op.paged_attn_sparse(b.q[: b.M], b.k, b.v, b.kmin, b.kmax, b.table, b.cu, b.ctx, b.page, *sel)["blocks"]
+        bl = blocks.cpu().numpy()[: b.M]
+        assert bl[0, 0].tolist() == list(range(sel[0] - sel[2])) + [b.ctx[0] // 16 - j for j in reversed(range(sel[2]))]
+        assert np.array_equal(bl, want)
+        o = out.float()
+        assert torch.isnan(o[0, 1]).all() and torch.isfinite(o[0, 0]).all() and torch.isfinite(o[1: b.M]).all()
