@@ -142,7 +142,11 @@ k_paged_plan(PagedArgs a, int units, int TM) {
   const int tid = threadIdx.x;
   const bool tiles = a.G * a.max_block > TM;
   if (tiles)
-    for (int j = tid; j < a.B; j += 1024) s_first[j] = run_tile(a.cu[j], a.G, TM, j);
+    for (int j = tid; j < a.B; j += 1024) {
+      ReqRows r;
+      paged_request(a, j, true, r);         // a refused request need not be any tile's
+      s_first[j] = run_tile(a.cu[j], a.G, TM, j);
+    }
   if (tid < 256) s_at[tid] = 0;
   __syncthreads();
   auto items = [&](bool report, auto emit) {
@@ -172,7 +176,7 @@ k_paged_plan(PagedArgs a, int units, int TM) {
       }
     }
   };
-  items(true, [&](int cls, int, int, int) { atomicAdd(&s_at[cls], 1); });
+  items(!tiles, [&](int cls, int, int, int) { atomicAdd(&s_at[cls], 1); });
   __syncthreads();
   int n = 0, x = 0;
   if (tid < 256) {                          // places: exclusive sum of the counts

@@ -175,6 +175,12 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, int idx, int units
     c = item.z;
   } else if (a.G * a.max_block > TM) {
     auto first_tile = [&](int j) { return run_tile(a.cu[j], a.G, TM, j); };
+    // a refused request need not be any tile's: the first workgroup looks at all of them
+    if (idx == 0)
+      for (int j = threadIdx.x; j < a.B; j += THREADS) {
+        ReqRows r;
+        paged_request(a, j, true, r);
+      }
     i = find_run<THREADS>(a.B, u, s_cnt, first_tile);
     if (i < 0) return false;
     r0 = ((long long)u - first_tile(i)) * TM;

@@ -924,3 +924,15 @@ def test_sparse_nan_queries():
         assert np.array_equal(bl, want)
         o = out.float()
         assert torch.isnan(o[0, 1]).all() and torch.isfinite(o[0, 0]).all() and torch.isfinite(o[1: b.M]).all()
+
+
+@pytest.mark.parametrize("max_rows", [64, 60000])
+def test_bad_row_counts_in_tiles(max_rows):
+    """A request that ends before it starts, in a launch of several tiles a request, listed longest first or not: its bit,
+    though no tile is its own."""
+    need_gpu()
+    b = Batch(n_q=8, n_kv=2, hd=64, page=16, d=[40, 2, 1], ctx=[100, 30, 7], seed=40, extra_rows=max_rows - 43)
+    b.dcu.copy_(torch.tensor([0, 40, 20, 20]))
+    b.run(lse=False)
+    torch.cuda.synchronize()
+    assert int(b.err.item()) == L.DERR_CAPACITY
