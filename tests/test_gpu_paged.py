@@ -936,3 +936,72 @@ def test_bad_row_counts_in_tiles(max_rows):
     b.run(lse=False)
     torch.cuda.synchronize()
     assert int(b.err.item()) == L.DERR_CAPACITY
+
+
+# Launches of more work items than are dispatched as they come (1024: requests' tiles x kv heads x pieces), whose items
+# are listed longest first.
+PLANNED = {
+    # 64 requests x 2 kv heads x up to 11 pieces of 128 keys
+    "decode": dict(n_q=8, n_kv=2, hd=128, page=16, d=[1] * 64, ctx=[(j * j * 37) % 1300 for j in range(64)]),
+    "verify": dict(n_q=8, n_kv=2, hd=64, page=32, d=[j % 9 for j in range(64)], ctx=[(j * 211) % 1300 for j in range(64)]),
+    # room for 20000 rows: 161 tiles of 128 (row, head) pairs x 8 kv heads, few of them with rows
+    "prompt": dict(n_q=8, n_kv=8, hd=64, page=16, d=[150, 0, 1, 97, 200], ctx=[0, 3, 500, 63, 10], extra_rows=20000 - 448),
+    # room for 10000 rows of 16 heads in groups of 4: 317 tiles x 4 kv heads
+    "groups": dict(n_q=16, n_kv=4, hd=128, page=64, d=[33, 1, 40, 0, 3], ctx=[100, 900, 0, 5, 301], extra_rows=10000 - 77),
+}
+
+
+@pytest.mark.parametrize("name", list(PLANNED))
+def test_attn_listed_longest_first(name):
+    need_gpu()
+    b = Batch(seed=41, **PLANNED[name])
+    out, ls = b.run()
+    b.check(out, ls, b.oracle(), what=name)
+    assert int(b.err.item()) == 0
+    again, ls2 = b.run()
+    assert torch.equal(out, again) and torch.equal(ls, ls2)
+
+
+def test_attn_pieces_of_2048_keys():
+    """As many (request, kv head) pairs as work items are aimed at: a request's pieces are cut at 2048 keys, here up to 69
+    of them, more than the merge takes at a time."""
+    need_gpu()
+    ctx = [140000, 5000, 2046, 2047, 2048, 4095, 4096] + [j % 40 for j in range(1529)]
+    b = Batch(n_q=2, n_kv=1, hd=64, page=64, d=[1] * len(ctx), ctx=ctx, seed=42)
+    out, ls = b.run()
+    b.check(out, ls, b.oracle(), what="pieces")
+    assert int(b.err.item()) == 0
+
+
+@pytest.mark.parametrize("name", ["decode", "verify", "wide", "group64", "prompt", "prompt64"])
+def test_bounds_far_above_the_batch(name):
+    """One launch serves every batch within its bounds: contexts, blocks and row counts far below them."""
+    need_gpu()
+    b = Batch(seed=43, extra_rows=700, **ATTN[name])
+    for kw in (dict(max_ctx=100000), dict(max_block=64 if b.max_block < 64 else 1000, max_ctx=70000)):
+        out, ls = b.run(cfg=b.cfg(**kw))
+        b.check(out, ls, b.oracle(), what=f"{name} {kw}")
+        assert int(b.err.item()) == 0
+
+
+@pytest.mark.parametrize("name,listed", [("wide", False), ("prompt", False), ("prompt", True), ("prompt64", False), ("prompt64", True)])
+def test_bad_device_data_in_tiles(name, listed):
+    """A fault of one request sets its bit and leaves the other requests' rows bitwise unchanged: wide tiles, dispatched as
+    they come and listed longest first."""
+    need_gpu()
+    shape = ATTN[name]
+    i = 2
+    spoils = [(L.DERR_PAGE, lambda b: b.dtable.__setitem__((i, 0), -1)),
+              (L.DERR_PAGE, lambda b: b.dtable.__setitem__((i, int(b.ctx[i] + b.d[i] - 1) // b.page), b.k.shape[0])),
+              (L.DERR_CAPACITY, lambda b: b.dctx.__setitem__(i, -1)),
+              (L.DERR_CAPACITY, lambda b: b.dctx.__setitem__(i, 2 ** 31 - 1))]
+    for bit, spoil in spoils:
+        b = Batch(seed=44, extra_rows=40000 if listed else 3, **shape)
+        want, _ = b.run()
+        assert int(b.err.item()) == 0
+        spoil(b)
+        got, _ = b.run()
+        torch.cuda.synchronize()
+        others = torch.tensor([t for t in range(b.M) if not b.cu[i] <= t < b.cu[i + 1]], device="cuda")
+        assert int(b.err.item()) == bit
+        assert torch.equal(want[others], got[others]) and (got[b.M:] == 7.0).all()
