@@ -166,3 +166,59 @@ def test_oracle_closed_forms():
     score = np.maximum(qs, 0).sum(0) @ kk.max(1).T + np.minimum(qs, 0).sum(0) @ kk.min(1).T
     assert ((kk @ qs.sum(0)).max(1) <= score).all()
     assert op.select_pages(qs, kk.min(1), kk.max(1), 3, 1, 1) == sorted({0, 4, 1 + int(np.argmax(score[1:4]))})
+
+
+# The calls below get as far as the check that is tried, or to a refusal of tensors that are not on a GPU: nothing is launched.
+
+def _tensors(**kw):
+    """A cache of 2 kv heads, pages of 16, head_dim 64, and the arguments of a batch of 4 with 6 rows, 4 query heads."""
+    t = dict(k=torch.zeros(8, 2, 16, 64, dtype=torch.bfloat16), v=torch.zeros(8, 2, 16, 64, dtype=torch.bfloat16),
+             table=torch.zeros(4, 5, dtype=torch.int32), kmin=torch.zeros(8, 2, 64, dtype=torch.bfloat16),
+             kmax=torch.zeros(8, 2, 64, dtype=torch.bfloat16), q=torch.zeros(6, 4, 64, dtype=torch.bfloat16),
+             cu=torch.zeros(5, dtype=torch.int32), ctx=torch.zeros(4, dtype=torch.int32), pos=torch.zeros(6, dtype=torch.int32),
+             req=torch.zeros(6, dtype=torch.int32), nk=torch.zeros(6, 128, dtype=torch.bfloat16),
+             nv=torch.zeros(6, 128, dtype=torch.bfloat16), out=torch.zeros(6, 4, 64, dtype=torch.bfloat16), lse=torch.zeros(6, 4),
+             err=torch.zeros(1, dtype=torch.int32), ws=torch.zeros(1 << 20, dtype=torch.uint8),
+             gcu=torch.zeros(2, dtype=torch.int32), pre=torch.zeros(1, dtype=torch.int32), blocks=torch.zeros(6, 2, 3, dtype=torch.int32))
+    t.update(kw)
+    return t
+
+
+CALLS = {
+    "append": lambda c, p, t: L.paged_append(c, p, 4, t["cu"], t["pos"], t["req"], t["q"], t["nk"], t["nv"], t["out"], 1e4, dev_err=t["err"]),
+    "attn": lambda c, p, t: L.paged_attn(c, p, 4, t["q"], t["cu"], t["ctx"], t["out"], t["ws"], lse=t["lse"], dev_err=t["err"]),
+    "attn_shared": lambda c, p, t: L.paged_attn_shared(c, p, 4, t["q"], t["cu"], t["ctx"], t["out"], t["ws"], t["gcu"], t["pre"],
+                                                       lse=t["lse"], dev_err=t["err"]),
+    "attn_sparse": lambda c, p, t: L.paged_attn_sparse(c, p, 4, t["q"], t["cu"], t["ctx"], t["out"], t["ws"], 3, 1, 1, blocks=t["blocks"],
+                                                       lse=t["lse"], dev_err=t["err"]),
+}
+
+
+def _small_cfg(**kw):
+    return _cfg(**{**dict(n_q=4, n_kv=2, head_dim=64, page=16, max_ctx=80, max_block=2, max_rows=6), **kw})
+
+
+def _refused(call, why, cfg=None, **kw):
+    t = _tensors(**kw)
+    pages = L.pages_desc(t["k"], t["v"], t["table"], t["kmin"], t["kmax"])
+    with pytest.raises(L.DcutError, match=f"dcut_paged_{call}, {why}:"):
+        CALLS[call](_small_cfg() if cfg is None else cfg, pages, t)
+
+
+def test_pools_of_other_types_and_shapes_are_refused():
+    good = _tensors()
+    desc = lambda **kw: L.pages_desc(*[{**good, **kw}[n] for n in ("k", "v", "table", "kmin", "kmax")])
+    desc()
+    desc(kmin=None, kmax=None)
+    desc(**{n: good[n].view(torch.int16) for n in ("k", "v", "kmin", "kmax")})
+    for bad in (dict(k=good["k"].half(), v=good["v"].half()), dict(v=good["v"].half()), dict(k=good["k"].float(), v=good["v"].float()),
+                dict(k=good["k"][0], v=good["v"][0]), dict(kmin=good["kmin"].float()), dict(kmax=good["kmax"][:7]),
+                dict(kmin=good["kmin"].flatten(1)), dict(table=good["table"].long()), dict(table=good["table"][0])):
+        with pytest.raises(L.DcutError):
+            desc(**bad)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+def test_pools_that_do_not_match_the_configuration_are_refused(call):
+    for kw in (dict(page=32), dict(n_kv=1), dict(n_kv=4), dict(head_dim=128)):
+        _refused(call, "pool", cfg=_small_cfg(**kw))
