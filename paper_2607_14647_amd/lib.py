@@ -304,29 +304,36 @@ def paged_cfg(n_q: int, n_kv: int, head_dim: int, page: int, max_ctx: int, max_b
 
 def pages_desc(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kmin: Optional[torch.Tensor] = None,
                kmax: Optional[torch.Tensor] = None) -> Pages:
-    """Descriptor of a paged cache: k, v [n_pages][n_kv][page][head_dim], table [B][columns] int32 (its rows may be
-    strided), channel bounds kmin, kmax [n_pages][n_kv][head_dim] or None; all but the table bf16 (also as raw 16-bit
-    integers).  The descriptor keeps the tensors alive."""
+    """Descriptor of a paged cache: k, v [n_pages][n_kv][page][head_dim], table [B][columns] int32, channel bounds kmin,
+    kmax [n_pages][n_kv][head_dim] or None; all but the table bf16 (also as raw 16-bit integers).  The descriptor keeps
+    the tensors alive.  The table may be a view of some columns of a wider one: the library knows its row stride only,
+    so the calls then refuse a max_ctx of more keys than these columns hold."""
     p = lambda t: t.data_ptr() if t is not None else None
     pool = [t for t in (k, v, kmin, kmax) if t is not None]
     if not all(t.is_contiguous() and _ELEMENTS.get(t.dtype) == BF16 for t in pool) or v.shape != k.shape or k.dim() != 4:
         raise DcutError(EINVAL, "pages_desc, pool")
     if any(t.shape != k.shape[:2] + k.shape[3:] for t in (kmin, kmax) if t is not None):
         raise DcutError(EINVAL, "pages_desc, channel bounds")
-    if table.dtype is not torch.int32 or table.dim() != 2 or table.stride(1) != 1:
+    if table.dtype is not torch.int32 or table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] != 1):
         raise DcutError(EINVAL, "pages_desc, table")
+    ld = table.stride(0) if table.shape[0] > 1 else table.shape[1]
     if any(t.device != k.device for t in pool + [table]):
         raise DcutError(EINVAL, "pages_desc, device")
-    desc = Pages(p(k), p(v), p(table), k.shape[0], table.stride(0), p(kmin), p(kmax))
+    desc = Pages(p(k), p(v), p(table), k.shape[0], ld, p(kmin), p(kmax))
     desc.tensors = (k, v, table, kmin, kmax)
-    desc.pool = tuple(k.shape[1:])
+    desc.pool, desc.rows = tuple(k.shape[1:]), table.shape[0]
+    desc.max_ctx = table.shape[1] * k.shape[2] if ld > table.shape[1] else None
     return desc
 
 
-def _pages(call: str, cfg: PagedCfg, pages: Pages):
-    """The descriptor, whose pool (where it was made from tensors) is one of the configuration's shape."""
-    if getattr(pages, "pool", None) not in ((cfg.n_kv, cfg.page, cfg.head_dim), None):
-        raise DcutError(EINVAL, f"{call}, pool")
+def _pages(call: str, cfg: PagedCfg, pages: Pages, B: int):
+    """The descriptor; one made from tensors has a pool of the configuration's shape and a table that reaches as far as
+    the batch and the contexts may."""
+    if getattr(pages, "pool", None) is not None:
+        if pages.pool != (cfg.n_kv, cfg.page, cfg.head_dim):
+            raise DcutError(EINVAL, f"{call}, pool")
+        if B > pages.rows or (pages.max_ctx is not None and cfg.max_ctx > pages.max_ctx):
+            raise DcutError(EINVAL, f"{call}, table")
     return C.byref(pages)
 
 
@@ -347,7 +354,7 @@ def paged_append(cfg: PagedCfg, pages: Pages, B: int, cu: torch.Tensor, packed_p
     kind = _ELEMENTS.get(dtype)
     if kind is None or v.dtype is not dtype or (q is not None and q.dtype is not dtype):
         raise DcutError(EINVAL, "dcut_paged_append")
-    st = _lib.dcut_paged_append(C.byref(cfg), _pages("dcut_paged_append", cfg, pages), B, _p(cu), _p(packed_pos), _p(packed_req),
+    st = _lib.dcut_paged_append(C.byref(cfg), _pages("dcut_paged_append", cfg, pages, B), B, _p(cu), _p(packed_pos), _p(packed_req),
                                 kind, _p(q), q.stride(0) if q is not None else 0,
                                 _p(k), k.stride(0), _p(v), v.stride(0), float(theta), _p(q_out), _p(dev_err),
                                 _stream(stream))
@@ -357,7 +364,7 @@ def paged_append(cfg: PagedCfg, pages: Pages, B: int, cu: torch.Tensor, packed_p
 def paged_attn(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
                out: torch.Tensor, ws: Optional[torch.Tensor], lse: Optional[torch.Tensor] = None,
                dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
-    st = _lib.dcut_paged_attn(C.byref(cfg), _pages("dcut_paged_attn", cfg, pages), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), _p(out), _p(lse),
+    st = _lib.dcut_paged_attn(C.byref(cfg), _pages("dcut_paged_attn", cfg, pages, B), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), _p(out), _p(lse),
                               _p(dev_err), _p(ws), ws.numel() * ws.element_size() if ws is not None else 0,
                               _stream(stream))
     _check(st, "dcut_paged_attn")
@@ -368,7 +375,7 @@ def paged_attn_shared(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: 
                       lse: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
     if group_cu.numel() != prefix_len.numel() + 1:
         raise DcutError(EINVAL, "dcut_paged_attn_shared")
-    st = _lib.dcut_paged_attn_shared(C.byref(cfg), _pages("dcut_paged_attn_shared", cfg, pages), B, _p(q), q.stride(0), _p(cu), _p(ctx_len),
+    st = _lib.dcut_paged_attn_shared(C.byref(cfg), _pages("dcut_paged_attn_shared", cfg, pages, B), B, _p(q), q.stride(0), _p(cu), _p(ctx_len),
                                      prefix_len.numel(), _p(group_cu), _p(prefix_len), _p(out), _p(lse), _p(dev_err),
                                      _p(ws), ws.numel() * ws.element_size(), _stream(stream))
     _check(st, "dcut_paged_attn_shared")
@@ -378,7 +385,7 @@ def paged_attn_sparse(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: 
                       out: torch.Tensor, ws: torch.Tensor, n_sel: int, n_sink: int, n_local: int,
                       blocks: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                       dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
-    st = _lib.dcut_paged_attn_sparse(C.byref(cfg), _pages("dcut_paged_attn_sparse", cfg, pages), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), int(n_sel),
+    st = _lib.dcut_paged_attn_sparse(C.byref(cfg), _pages("dcut_paged_attn_sparse", cfg, pages, B), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), int(n_sel),
                                      int(n_sink), int(n_local), _p(blocks), _p(out), _p(lse), _p(dev_err), _p(ws),
                                      ws.numel() * ws.element_size(), _stream(stream))
     _check(st, "dcut_paged_attn_sparse")

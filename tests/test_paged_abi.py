@@ -222,3 +222,18 @@ def test_pools_of_other_types_and_shapes_are_refused():
 def test_pools_that_do_not_match_the_configuration_are_refused(call):
     for kw in (dict(page=32), dict(n_kv=1), dict(n_kv=4), dict(head_dim=128)):
         _refused(call, "pool", cfg=_small_cfg(**kw))
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+def test_tables_that_end_before_the_batch_does_are_refused(call):
+    """Fewer rows than requests; a view of fewer columns than its row stride, where max_ctx reaches into the others."""
+    wide = torch.zeros(4, 9, dtype=torch.int32)
+    _refused(call, "table", table=wide[:3])
+    for view in (wide[:, :4], wide[:, 5:]):
+        _refused(call, "table", table=view)                             # max_ctx 80: five columns
+        assert L.pages_desc(_tensors()["k"], _tensors()["v"], view).max_ctx == 64
+    # a row of its own has no stride to go by
+    one = L.pages_desc(_tensors()["k"], _tensors()["v"], wide[1:2, 2:6])
+    assert (one.table_ld, one.max_ctx) == (4, None)
+    # nor has a single column: one page a request
+    assert L.pages_desc(_tensors()["k"], _tensors()["v"], torch.zeros(1, 4, dtype=torch.int32).t()).table_ld == 1
