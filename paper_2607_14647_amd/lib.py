@@ -321,20 +321,63 @@ def pages_desc(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kmin: Opti
         raise DcutError(EINVAL, "pages_desc, device")
     desc = Pages(p(k), p(v), p(table), k.shape[0], ld, p(kmin), p(kmax))
     desc.tensors = (k, v, table, kmin, kmax)
-    desc.pool, desc.rows = tuple(k.shape[1:]), table.shape[0]
     desc.max_ctx = table.shape[1] * k.shape[2] if ld > table.shape[1] else None
+    desc.made = (*k.shape[1:], table.shape[0], desc.max_ctx or 2 ** 31, k.get_device())
     return desc
 
 
-def _pages(call: str, cfg: PagedCfg, pages: Pages, B: int):
-    """The descriptor; one made from tensors has a pool of the configuration's shape and a table that reaches as far as
-    the batch and the contexts may."""
-    if getattr(pages, "pool", None) is not None:
-        if pages.pool != (cfg.n_kv, cfg.page, cfg.head_dim):
-            raise DcutError(EINVAL, f"{call}, pool")
-        if B > pages.rows or (pages.max_ctx is not None and cfg.max_ctx > pages.max_ctx):
-            raise DcutError(EINVAL, f"{call}, table")
-    return C.byref(pages)
+# What the library cannot see behind a pointer.  A call's tensors are checked as their pointers are taken: element type,
+# elements one after the other (rows of q, k and v: within a row), and the device, which has to be the current one.
+
+def _pages(call: str, cfg: PagedCfg, pages: Pages, B: int) -> int:
+    """The descriptor's device.  One made from tensors has a pool of the configuration's shape and a table that reaches
+    as far as the batch and the contexts may."""
+    made = getattr(pages, "made", None)
+    if made is None:
+        return torch.cuda.current_device()
+    n_kv, page, head_dim, rows, max_ctx, dev = made
+    if cfg.n_kv != n_kv or cfg.page != page or cfg.head_dim != head_dim:
+        raise DcutError(EINVAL, f"{call}, pool")
+    if B > rows or cfg.max_ctx > max_ctx:
+        raise DcutError(EINVAL, f"{call}, table")
+    return dev
+
+
+def _array(call: str, name: str, t: torch.Tensor, dev: int, dtype=torch.int32):
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise DcutError(EINVAL, f"{call}, {name}")
+    return t.data_ptr()
+
+
+def _halves(call: str, name: str, t: torch.Tensor, dev: int):
+    if _ELEMENTS.get(t.dtype) != BF16 or t.get_device() != dev or not t.is_contiguous():
+        raise DcutError(EINVAL, f"{call}, {name}")
+    return t.data_ptr()
+
+
+def _row_stride(call: str, name: str, t: torch.Tensor, width: int, dev: int) -> int:
+    """Stride of rows of `width` elements."""
+    if t.get_device() != dev:
+        raise DcutError(EINVAL, f"{call}, {name}")
+    stride, shape = t.stride(), t.shape
+    if len(stride) == 2 and stride[1] == 1 and shape[1] == width and shape[0] != 1:        # the usual ones first
+        return stride[0]
+    if len(stride) > 1 and t.is_contiguous() and t.numel() == shape[0] * width:
+        return width
+    at = 1
+    for n, step in zip(shape[:0:-1], stride[:0:-1]):
+        if step != at and n != 1:
+            raise DcutError(EINVAL, f"{call}, {name}")
+        at *= n
+    if at != width:
+        raise DcutError(EINVAL, f"{call}, {name}")
+    return stride[0] if shape[0] != 1 else width
+
+
+def _stream_on(call: str, dev: int, stream):
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise DcutError(EINVAL, f"{call}, device")
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def paged_workspace_bytes(call: str, cfg: PagedCfg, B: int, n_sel: int = 0) -> int:
@@ -349,46 +392,74 @@ def paged_append(cfg: PagedCfg, pages: Pages, B: int, cu: torch.Tensor, packed_p
                  packed_req: torch.Tensor, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                  q_out: Optional[torch.Tensor], theta: float, dev_err: Optional[torch.Tensor] = None,
                  stream=None) -> None:
-    """q, k, v: [rows][...] of float32 or bf16 (also as raw 16-bit integers), rows of any stride."""
-    dtype = k.dtype
+    """q, k, v: [rows][...] of float32 or bf16 (also as raw 16-bit integers), one type, rows of any stride."""
+    call, dtype = "dcut_paged_append", k.dtype
     kind = _ELEMENTS.get(dtype)
     if kind is None or v.dtype is not dtype or (q is not None and q.dtype is not dtype):
-        raise DcutError(EINVAL, "dcut_paged_append")
-    st = _lib.dcut_paged_append(C.byref(cfg), _pages("dcut_paged_append", cfg, pages, B), B, _p(cu), _p(packed_pos), _p(packed_req),
-                                kind, _p(q), q.stride(0) if q is not None else 0,
-                                _p(k), k.stride(0), _p(v), v.stride(0), float(theta), _p(q_out), _p(dev_err),
-                                _stream(stream))
-    _check(st, "dcut_paged_append")
+        raise DcutError(EINVAL, call)
+    dev = _pages(call, cfg, pages, B)
+    width, q_p, ldq = cfg.n_kv * cfg.head_dim, None, 0
+    if q is not None:
+        q_p, ldq = q.data_ptr(), _row_stride(call, "q", q, cfg.n_q * cfg.head_dim, dev)
+    ldk, ldv = _row_stride(call, "k", k, width, dev), _row_stride(call, "v", v, width, dev)
+    if cu.numel() <= B:
+        raise DcutError(EINVAL, f"{call}, cu")
+    st = _lib.dcut_paged_append(cfg, pages, B, _array(call, "cu", cu, dev), _array(call, "packed_pos", packed_pos, dev),
+                                _array(call, "packed_req", packed_req, dev), kind, q_p, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                theta, None if q_out is None else _halves(call, "q_out", q_out, dev),
+                                None if dev_err is None else _array(call, "dev_err", dev_err, dev), _stream_on(call, dev, stream))
+    _check(st, call)
+
+
+def _attn_args(call: str, cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
+               out: torch.Tensor, lse: Optional[torch.Tensor], dev_err: Optional[torch.Tensor], ws: Optional[torch.Tensor]):
+    """Device, first arguments (up to the contexts) and last ones (output to scratch) of an attention call."""
+    dev = _pages(call, cfg, pages, B)
+    if _ELEMENTS.get(q.dtype) != BF16:
+        raise DcutError(EINVAL, f"{call}, q")
+    ldq = _row_stride(call, "q", q, cfg.n_q * cfg.head_dim, dev)
+    if cu.numel() <= B or ctx_len.numel() < B:
+        raise DcutError(EINVAL, f"{call}, {'cu' if cu.numel() <= B else 'ctx_len'}")
+    nbytes = 0
+    if ws is not None:
+        if ws.get_device() != dev or not ws.is_contiguous():
+            raise DcutError(EINVAL, f"{call}, ws")
+        nbytes = ws.numel() * ws.element_size()
+    first = (cfg, pages, B, q.data_ptr(), ldq, _array(call, "cu", cu, dev), _array(call, "ctx_len", ctx_len, dev))
+    return dev, first, (_halves(call, "out", out, dev), None if lse is None else _array(call, "lse", lse, dev, torch.float32),
+                        None if dev_err is None else _array(call, "dev_err", dev_err, dev), _p(ws), nbytes)
 
 
 def paged_attn(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
                out: torch.Tensor, ws: Optional[torch.Tensor], lse: Optional[torch.Tensor] = None,
                dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
-    st = _lib.dcut_paged_attn(C.byref(cfg), _pages("dcut_paged_attn", cfg, pages, B), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), _p(out), _p(lse),
-                              _p(dev_err), _p(ws), ws.numel() * ws.element_size() if ws is not None else 0,
-                              _stream(stream))
-    _check(st, "dcut_paged_attn")
+    """q: [rows][...] bf16 (also as raw 16-bit integers), rows of any stride; the outputs are contiguous."""
+    call = "dcut_paged_attn"
+    dev, first, last = _attn_args(call, cfg, pages, B, q, cu, ctx_len, out, lse, dev_err, ws)
+    _check(_lib.dcut_paged_attn(*first, *last, _stream_on(call, dev, stream)), call)
 
 
 def paged_attn_shared(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
                       out: torch.Tensor, ws: torch.Tensor, group_cu: torch.Tensor, prefix_len: torch.Tensor,
                       lse: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
-    if group_cu.numel() != prefix_len.numel() + 1:
-        raise DcutError(EINVAL, "dcut_paged_attn_shared")
-    st = _lib.dcut_paged_attn_shared(C.byref(cfg), _pages("dcut_paged_attn_shared", cfg, pages, B), B, _p(q), q.stride(0), _p(cu), _p(ctx_len),
-                                     prefix_len.numel(), _p(group_cu), _p(prefix_len), _p(out), _p(lse), _p(dev_err),
-                                     _p(ws), ws.numel() * ws.element_size(), _stream(stream))
-    _check(st, "dcut_paged_attn_shared")
+    call, n = "dcut_paged_attn_shared", prefix_len.numel()
+    if group_cu.numel() != n + 1:
+        raise DcutError(EINVAL, call)
+    dev, first, last = _attn_args(call, cfg, pages, B, q, cu, ctx_len, out, lse, dev_err, ws)
+    st = _lib.dcut_paged_attn_shared(*first, n, _array(call, "group_cu", group_cu, dev),
+                                     _array(call, "prefix_len", prefix_len, dev), *last, _stream_on(call, dev, stream))
+    _check(st, call)
 
 
 def paged_attn_sparse(cfg: PagedCfg, pages: Pages, B: int, q: torch.Tensor, cu: torch.Tensor, ctx_len: torch.Tensor,
                       out: torch.Tensor, ws: torch.Tensor, n_sel: int, n_sink: int, n_local: int,
                       blocks: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                       dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
-    st = _lib.dcut_paged_attn_sparse(C.byref(cfg), _pages("dcut_paged_attn_sparse", cfg, pages, B), B, _p(q), q.stride(0), _p(cu), _p(ctx_len), int(n_sel),
-                                     int(n_sink), int(n_local), _p(blocks), _p(out), _p(lse), _p(dev_err), _p(ws),
-                                     ws.numel() * ws.element_size(), _stream(stream))
-    _check(st, "dcut_paged_attn_sparse")
+    call = "dcut_paged_attn_sparse"
+    dev, first, last = _attn_args(call, cfg, pages, B, q, cu, ctx_len, out, lse, dev_err, ws)
+    st = _lib.dcut_paged_attn_sparse(*first, int(n_sel), int(n_sink), int(n_local),
+                                     None if blocks is None else _array(call, "blocks", blocks, dev), *last, _stream_on(call, dev, stream))
+    _check(st, call)
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:

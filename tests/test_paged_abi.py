@@ -237,3 +237,44 @@ def test_tables_that_end_before_the_batch_does_are_refused(call):
     assert (one.table_ld, one.max_ctx) == (4, None)
     # nor has a single column: one page a request
     assert L.pages_desc(_tensors()["k"], _tensors()["v"], torch.zeros(1, 4, dtype=torch.int32).t()).table_ld == 1
+
+
+WRONG = dict(cu=[lambda x: x.long(), lambda x: x[:4], lambda x: x.repeat(2)[::2]], ctx=[lambda x: x.long(), lambda x: x[:3]],
+             pos=[lambda x: x.long(), lambda x: x.repeat(2)[::2]], req=[lambda x: x.long()],
+             q=[lambda x: x.float(), lambda x: x.half(), lambda x: x[..., :32], lambda x: x[:, :3], lambda x: x.transpose(1, 2),
+                lambda x: x.transpose(1, 2).contiguous().transpose(1, 2), lambda x: torch.cat([x, x], 2)[..., ::2], lambda x: x.flatten()],
+             nk=[lambda x: x[:, :64], lambda x: torch.cat([x, x], 1)[:, ::2]], nv=[lambda x: x[:, :64], lambda x: x.t().contiguous().t()],
+             out=[lambda x: x.float(), lambda x: x.repeat(1, 2, 1)[:, :4]], lse=[lambda x: x.bfloat16(), lambda x: x.repeat(1, 2)[:, :4]],
+             err=[lambda x: x.long()], ws=[lambda x: x[::2]], gcu=[lambda x: x.long()], pre=[lambda x: x.long()],
+             blocks=[lambda x: x.long(), lambda x: x.transpose(1, 2)])
+NAMES = dict(cu="cu", ctx="ctx_len", pos="packed_pos", req="packed_req", nk="k", nv="v", out="out", err="dev_err", gcu="group_cu",
+             pre="prefix_len")
+USED = dict(append=("cu", "pos", "req", "q", "nk", "nv", "out", "err"), attn=("q", "cu", "ctx", "out", "lse", "err", "ws"))
+USED["attn_shared"], USED["attn_sparse"] = USED["attn"] + ("gcu", "pre"), USED["attn"] + ("blocks",)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+def test_tensors_of_other_types_and_strides_are_refused(call):
+    """A wrong element type, elements that do not follow each other, too few of them: refused by name."""
+    good = _tensors()
+    for name in USED[call]:
+        why = "q_out" if (call, name) == ("append", "out") else NAMES.get(name, name)
+        for wrong in WRONG[name]:
+            bad = wrong(good[name])
+            if call == "append" and name == "q" and bad.dtype is not torch.bfloat16:
+                continue                   # of another type than k and v, refused as before
+            _refused(call, why, **{name: bad})
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+def test_rows_may_lie_apart(call):
+    """Views of a fused projection, further dimensions, a single row of any stride: nothing is left to refuse but the
+    device, on which the cache has to be."""
+    x = torch.zeros(6, 512 + 8, dtype=torch.bfloat16)
+    raw = lambda t: t.view(torch.int16)
+    for kw in ({}, dict(q=x[:, :256], nk=x[:, 256:384], nv=x[:, 384:512]), dict(q=x[:, :256].view(6, 2, 2, 64)),
+               dict(q=torch.zeros(4, 1, 64, dtype=torch.bfloat16).transpose(0, 1)),
+               dict(q=raw(x)[:, :256], nk=raw(x)[:, 256:384], nv=raw(x)[:, 384:512], out=raw(_tensors()["out"]))):
+        _refused(call, "device", **kw)
+    wide = torch.zeros(4, 9, dtype=torch.int32)
+    _refused(call, "device", cfg=_small_cfg(max_ctx=64), table=wide[:, :4])
