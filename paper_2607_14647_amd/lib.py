@@ -406,7 +406,7 @@ def paged_append(cfg: PagedCfg, pages: Pages, B: int, cu: torch.Tensor, packed_p
         raise DcutError(EINVAL, f"{call}, cu")
     st = _lib.dcut_paged_append(cfg, pages, B, _array(call, "cu", cu, dev), _array(call, "packed_pos", packed_pos, dev),
                                 _array(call, "packed_req", packed_req, dev), kind, q_p, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                theta, None if q_out is None else _halves(call, "q_out", q_out, dev),
+                                float(theta), None if q_out is None else _halves(call, "q_out", q_out, dev),
                                 None if dev_err is None else _array(call, "dev_err", dev_err, dev), _stream_on(call, dev, stream))
     _check(st, call)
 

@@ -278,3 +278,13 @@ def test_rows_may_lie_apart(call):
         _refused(call, "device", **kw)
     wide = torch.zeros(4, 9, dtype=torch.int32)
     _refused(call, "device", cfg=_small_cfg(max_ctx=64), table=wide[:, :4])
+
+
+@pytest.mark.parametrize("theta", [-1, -1.0, np.float32(-1), np.float64(-1), torch.tensor(-1.0)])
+def test_rotation_bases_of_any_number_type(theta, monkeypatch):
+    """They reach the library, which refuses this one by its value."""
+    monkeypatch.setattr(L, "_stream_on", lambda *a: None)
+    t = _tensors()
+    pages = L.pages_desc(t["k"], t["v"], t["table"], t["kmin"], t["kmax"])
+    with pytest.raises(L.DcutError, match="dcut_paged_append:"):
+        L.paged_append(_small_cfg(), pages, 4, t["cu"], t["pos"], t["req"], t["q"], t["nk"], t["nv"], t["out"], theta)
