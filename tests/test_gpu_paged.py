@@ -1005,3 +1005,28 @@ def test_bad_device_data_in_tiles(name, listed):
         others = torch.tensor([t for t in range(b.M) if not b.cu[i] <= t < b.cu[i + 1]], device="cuda")
         assert int(b.err.item()) == bit
         assert torch.equal(want[others], got[others]) and (got[b.M:] == 7.0).all()
+
+
+@pytest.mark.parametrize("name,call", [("verify", "attn"), ("wide", "attn"), ("prompt64", "attn"), ("verify", "sparse"), ("tiles", "shared"),
+                                       ("groups", "shared")])
+def test_rows_without_a_finite_score(name, call):
+    """Every score of some rows is minus infinity: they give 0 and a log sum of minus infinity, the other rows what they
+    gave."""
+    need_gpu()
+    shape, groups = SHARED[name] if call == "shared" else (ATTN[name], ())
+    b = Batch(seed=45, prefix=groups, **shape)
+    q = b.dq.view(b.rows, b.n_q, b.hd)
+    q[:, :, 7] = 0.0                               # the channel in which the rows below differ from the others
+    b.k[..., 7] = bf(np.array(-1e38))
+    b.dk[..., 7] = -1e38
+    b.bounds()
+    kw = dict(groups=_groups(b, groups)) if call == "shared" else dict(sel=(4, 1, 1)) if call == "sparse" else {}
+    want, wls = b.run(call, **kw)
+    rows = torch.tensor([t for t in range(b.M) if t % 3 == 1], device="cuda")
+    others = torch.tensor([t for t in range(b.M) if t % 3 != 1], device="cuda")
+    q[rows, :, 7] = 1e38
+    out, ls = b.run(call, **kw)
+    torch.cuda.synchronize()
+    assert (out[rows] == 0).all() and torch.isneginf(ls[rows]).all()
+    assert torch.equal(out[others], want[others]) and torch.equal(ls[others], wls[others])
+    assert torch.isfinite(wls[: b.M]).all() and int(b.err.item()) == 0
