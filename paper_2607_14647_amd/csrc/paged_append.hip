@@ -5,10 +5,10 @@
 // table[i][p / page].  Angles, sines and cosines are formed in 64 bits (a far position
 // turns its fastest pair many times), the rotation in 32, one rounding to bf16 at the end.
 //
-// Bound by HBM: every element is read and written once.  A workgroup takes ROWS rows; its
-// threads first form the rows' sines and cosines in LDS, then walk the rows' 16-byte pieces.
-// 8 prompts of about 1000 rows (178 MB) 37 us with one row a workgroup, and 10 for the bounds, 3.9 TB/s
-// in all where a large copy reaches 4.8; with two and four rows a workgroup 41 and 42.
+// Bound by HBM: every element is read and written once.  A workgroup takes one row; its
+// threads first form the row's sines and cosines in LDS, then walk the row's 16-byte pieces.
+// 8 prompts of about 1000 rows (178 MB) 37 us, and 10 for the bounds, 3.9 TB/s in all where a
+// large copy reaches 4.8; two and four rows a workgroup took 41 and 42.
 // 64 single rows 4.4 us: a launch, two dependent loads and the sines.
 #include "paged.h"
 
@@ -42,76 +42,69 @@ __device__ __forceinline__ void store8(uint16_t *p, const float (&x)[8]) {
   *(uint4 *)p = make_uint4(pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3]), pack_bf2(x[4], x[5]), pack_bf2(x[6], x[7]));
 }
 
-template <int HD, typename T, int ROWS>
+template <int HD, typename T>
 __global__ void __launch_bounds__(256)
 k_paged_append(AppendArgs a) {
   constexpr int HALF = HD / 2, PP = HALF / 8, VP = HD / 8;   // 16-byte pairs of a head, 16-byte pieces of a value
-  __shared__ float2 s_cs[ROWS][HALF];
-  __shared__ long long s_slot[ROWS];        // element offset of (row's page, kv head 0, slot), or -1
-  const int tid = threadIdx.x;
-  const int r0 = blockIdx.x * ROWS;
-  const int end = a.cu[a.B], M = min(end, a.max_rows);
-  if (r0 >= M) {
+  __shared__ float2 s_cs[HALF];
+  __shared__ long long s_slot;              // element offset of (the row's page, kv head 0, slot), or -1
+  const int tid = threadIdx.x, t = blockIdx.x;
+  const int end = a.cu[a.B];
+  if (t >= min(end, a.max_rows)) {
     if (end < 0 && tid == 0 && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
     return;
   }
   const int page = 1 << a.lpage;
-  for (int e = tid; e < ROWS * HALF; e += 256) {
-    const int r = e / HALF, j = e - r * HALF;
-    if (r0 + r >= M) break;
-    const double ang = (double)a.pos[r0 + r] * exp2(-(2.0 * j / HD) * a.log2_theta);
+  if (tid < HALF) {
+    const double ang = (double)a.pos[t] * exp2(-(2.0 * tid / HD) * a.log2_theta);
     double sn, cs;
     sincos(ang, &sn, &cs);
-    s_cs[r][j] = make_float2((float)cs, (float)sn);
+    s_cs[tid] = make_float2((float)cs, (float)sn);
   }
-  if (tid < ROWS) {
+  if (tid == 0) {
     long long slot = -1;
-    if (r0 + tid < M) {
-      const int i = a.req[r0 + tid], p = a.pos[r0 + tid];
-      if (end > a.max_rows && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
-      if (i < 0 || i >= a.B || p < 0 || p >= a.max_ctx || (p >> a.lpage) >= a.table_ld) {
-        if (a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
+    const int i = a.req[t], p = a.pos[t];
+    if (end > a.max_rows && a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
+    if (i < 0 || i >= a.B || p < 0 || p >= a.max_ctx || (p >> a.lpage) >= a.table_ld) {
+      if (a.dev_err) atomicOr(a.dev_err, DCUT_DERR_CAPACITY);
+    } else {
+      const int pg = a.table[(size_t)i * a.table_ld + (p >> a.lpage)];
+      if ((unsigned)pg >= (unsigned)a.n_pages) {
+        if (a.dev_err) atomicOr(a.dev_err, DCUT_DERR_PAGE);
       } else {
-        const int pg = a.table[(size_t)i * a.table_ld + (p >> a.lpage)];
-        if ((unsigned)pg >= (unsigned)a.n_pages) {
-          if (a.dev_err) atomicOr(a.dev_err, DCUT_DERR_PAGE);
-        } else {
-          slot = (((long long)pg * a.n_kv) * page + (p & (page - 1))) * HD;
-        }
+        slot = (((long long)pg * a.n_kv) * page + (p & (page - 1))) * HD;
       }
     }
-    s_slot[tid] = slot;
+    s_slot = slot;
   }
   __syncthreads();
+  const long long slot = s_slot;
   const int nq = a.q ? a.n_q : 0;
-  const int per = (nq + a.n_kv) * PP + a.n_kv * VP;
+  const int pairs = (nq + a.n_kv) * PP, per = pairs + a.n_kv * VP;
   const long long head_step = (long long)page * HD;
-  for (int e = tid; e < ROWS * per; e += 256) {
-    const int r = e / per, w = e - r * per;
-    const int t = r0 + r;
-    if (t >= M) break;
-    if (w >= (nq + a.n_kv) * PP) {
-      const int u = w - (nq + a.n_kv) * PP, g = u / VP, j = 8 * (u - g * VP);
-      if (s_slot[r] < 0) continue;
+  for (int w = tid; w < per; w += 256) {
+    if (w >= pairs) {
+      const int u = w - pairs, g = u / VP, j = 8 * (u - g * VP);
+      if (slot < 0) continue;
       float x[8];
       load8((const T *)a.v + (size_t)t * a.ldv + g * HD + j, x);
-      store8(a.pv + s_slot[r] + g * head_step + j, x);
+      store8(a.pv + slot + g * head_step + j, x);
       continue;
     }
     const int h = w / PP, j = 8 * (w - h * PP);
     const bool key = h >= nq;
-    if (key && s_slot[r] < 0) continue;
+    if (key && slot < 0) continue;
     const T *src = key ? (const T *)a.k + (size_t)t * a.ldk + (h - nq) * HD : (const T *)a.q + (size_t)t * a.ldq + h * HD;
     float x1[8], x2[8];
     load8(src + j, x1);
     load8(src + j + HALF, x2);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const float2 y = rope_pair(x1[u], x2[u], s_cs[r][j + u]);
+      const float2 y = rope_pair(x1[u], x2[u], s_cs[j + u]);
       x1[u] = y.x;
       x2[u] = y.y;
     }
-    uint16_t *dst = key ? a.pk + s_slot[r] + (h - nq) * head_step : a.q_out + ((size_t)t * a.n_q + h) * HD;
+    uint16_t *dst = key ? a.pk + slot + (h - nq) * head_step : a.q_out + ((size_t)t * a.n_q + h) * HD;
     store8(dst + j, x1);
     store8(dst + j + HALF, x2);
   }
@@ -176,9 +169,7 @@ k_page_bounds(AppendArgs a, uint16_t *kmin, uint16_t *kmax) {
 
 template <int HD, typename T>
 int append_launch(const AppendArgs &a, const dcut_pages *pg, hipStream_t s) {
-  constexpr int ROWS = 1;
-  DCUT_TRY(launch(DCUT_KERNEL_PAGED_APPEND, k_paged_append<HD, T, ROWS>, dim3((a.max_rows + ROWS - 1) / ROWS), dim3(256), 0,
-                  s, a));
+  DCUT_TRY(launch(DCUT_KERNEL_PAGED_APPEND, k_paged_append<HD, T>, dim3(a.max_rows), dim3(256), 0, s, a));
   if (!pg->kmin) return DCUT_OK;
   return launch(DCUT_KERNEL_PAGED_BOUNDS, k_page_bounds<HD>, dim3((a.max_rows + BOUND_ROWS - 1) / BOUND_ROWS, a.n_kv), dim3(256), 0, s, a, pg->kmin, pg->kmax);
 }
