@@ -1030,3 +1030,27 @@ def test_rows_without_a_finite_score(name, call):
     assert (out[rows] == 0).all() and torch.isneginf(ls[rows]).all()
     assert torch.equal(out[others], want[others]) and torch.equal(ls[others], wls[others])
     assert torch.isfinite(wls[: b.M]).all() and int(b.err.item()) == 0
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("heads", [dict(n_q=4, n_kv=2, hd=64), dict(n_q=12, n_kv=2, hd=128), dict(n_q=64, n_kv=1, hd=64)])
+def test_every_page_size(page, heads):
+    """Each page size in every call, streamed and wide, with contexts and a prefix that end within a page."""
+    need_gpu()
+    P = 300
+    for d in ([1, 2, 0, 1], [40, 1, 33, 2]):
+        b = Batch(page=page, d=d, ctx=[P + 5, P + 260, P, P + 31], seed=46, prefix=[(0, 3, P)], **heads)
+        b.bounds()
+        ref = b.oracle()
+        out, ls = b.run()
+        b.check(out, ls, ref, what=f"page {page}")
+        g = (dev(np.array([0, 3]), torch.int32), dev(np.array([P]), torch.int32))
+        out, ls = b.run("shared", groups=g)
+        b.check(out, ls, ref, what=f"page {page} shared")
+        sel = (2, 0, 1)
+        blocks = torch.zeros(b.rows, b.n_kv, sel[0], dtype=torch.int32, device="cuda")
+        out, ls = b.run("sparse", sel=sel, blocks=blocks)
+        ref = op.paged_attn_sparse(b.q[: b.M], b.k, b.v, b.kmin, b.kmax, b.table, b.cu, b.ctx, b.page, *sel)
+        assert np.array_equal(blocks.cpu().numpy()[: b.M], ref["blocks"])
+        b.check(out, ls, ref, what=f"page {page} sparse")
+        assert int(b.err.item()) == 0
