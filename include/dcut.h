@@ -466,7 +466,8 @@ int dcut_paged_append(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B,
  *           aligned; calls that may overlap need scratch of their own
  *   dev_err DCUT_DERR_CAPACITY (rows or context outside the bounds or the table; the
  *           request's rows are unspecified), DCUT_DERR_PAGE
- * Rows from cu[B] on are neither read nor written.
+ * Rows before cu[0] and from cu[B] on are neither read nor written: a run of a
+ * batch's requests may be a call of its own, its rows numbered as in the batch.
  * Returns DCUT_OK, DCUT_EINVAL, DCUT_EUNSUPPORTED, DCUT_EWORKSPACE, DCUT_EHIP.
  */
 int dcut_paged_attn(const dcut_paged_cfg *cfg, const dcut_pages *pages, int B, const dcut_bf16 *q,

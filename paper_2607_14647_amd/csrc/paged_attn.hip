@@ -74,8 +74,8 @@ k_paged_merge(PagedArgs a) {
   const int pair = blockIdx.x * 4 + (threadIdx.x >> 6);
   const int t = pair / a.n_q;
   const int nc0 = a.row_nc[min(t, a.max_rows - 1)];
-  const int M = a.cu[a.B];
-  if (t >= M || t >= a.max_rows) return;
+  const int M0 = a.cu[0], M = a.cu[a.B];
+  if (t < M0 || t >= M || t >= a.max_rows) return;          // no request's row
   const int nc = min(nc0, a.MC);
   if (nc <= 1) return;
   const float *pp = a.part + ((size_t)pair * a.MC + odd) * ATTN_PITCH(HD);

@@ -1054,3 +1054,25 @@ def test_every_page_size(page, heads):
         assert np.array_equal(blocks.cpu().numpy()[: b.M], ref["blocks"])
         b.check(out, ls, ref, what=f"page {page} sparse")
         assert int(b.err.item()) == 0
+
+
+@pytest.mark.parametrize("call,shape", [("attn", dict(n_q=8, n_kv=2, hd=128, page=16, d=[2, 1, 3, 1], ctx=[300, 700, 500, 900])),
+                                        ("attn", dict(n_q=8, n_kv=2, hd=64, page=16, d=[2, 40, 3, 1], ctx=[300, 700, 500, 900])),
+                                        ("shared", dict(n_q=8, n_kv=2, hd=64, page=16, d=[2, 1, 3, 1], ctx=[300, 700, 500, 900])),
+                                        ("sparse", dict(n_q=8, n_kv=2, hd=64, page=16, d=[2, 1, 3, 1], ctx=[300, 700, 500, 900]))])
+def test_a_run_of_requests(call, shape):
+    """The requests from the second on in a call of their own, their rows numbered as in the whole batch (cu starts above
+    0): their rows are right, the first request's are neither read nor written."""
+    need_gpu()
+    b = Batch(seed=47, prefix=[(1, 4, 480)] if call == "shared" else (), **shape)
+    b.bounds()
+    sel = (30, 1, 1)
+    ref = (op.paged_attn_sparse(b.q[: b.M], b.k, b.v, b.kmin, b.kmax, b.table, b.cu, b.ctx, b.page, *sel) if call == "sparse"
+           else b.oracle())
+    b.dq[: int(b.d[0])] = float("nan")
+    b.dcu, b.dctx, b.dtable, b.B = b.dcu[1:], b.dctx[1:], b.dtable[1:], 3
+    kw = dict(sel=sel) if call == "sparse" else dict(groups=_groups(b, [(0, 3, 480)])) if call == "shared" else {}
+    out, ls = b.run(call, **kw)
+    b.check(out, ls, ref, rows=np.arange(int(b.d[0]), b.M), what=call)
+    n = int(b.d[0])
+    assert (out[:n] == 7.0).all() and (ls[:n] == 7.0).all() and int(b.err.item()) == 0
