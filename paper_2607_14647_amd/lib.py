@@ -1,4 +1,4 @@
-"""ctypes binding of libdcut.so (argument marshalling only).
+"""ctypes binding of libdcut.so (argument marshalling, and checks of the paged calls' tensors).
 
 Every function takes torch tensors that already live on the GPU and passes
 their device pointers, sizes and torch's current HIP stream to the C ABI in
@@ -322,7 +322,7 @@ def pages_desc(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kmin: Opti
     desc = Pages(p(k), p(v), p(table), k.shape[0], ld, p(kmin), p(kmax))
     desc.tensors = (k, v, table, kmin, kmax)
     desc.max_ctx = table.shape[1] * k.shape[2] if ld > table.shape[1] else None
-    desc.made = (*k.shape[1:], table.shape[0], desc.max_ctx or 2 ** 31, k.get_device())
+    desc.made = (*k.shape[1:], table.shape[0], 2 ** 31 if desc.max_ctx is None else desc.max_ctx, k.get_device())
     return desc
 
 

@@ -288,3 +288,8 @@ def test_rotation_bases_of_any_number_type(theta, monkeypatch):
     pages = L.pages_desc(t["k"], t["v"], t["table"], t["kmin"], t["kmax"])
     with pytest.raises(L.DcutError, match="dcut_paged_append:"):
         L.paged_append(_small_cfg(), pages, 4, t["cu"], t["pos"], t["req"], t["q"], t["nk"], t["nv"], t["out"], theta)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+def test_a_table_without_columns_is_refused(call):
+    _refused(call, "table", table=torch.zeros(4, 9, dtype=torch.int32)[:, :0])
