@@ -64,8 +64,8 @@ k_paged_shared(PagedArgs a, int pre_units, int pre_items, int units) {
 // Merge of a (row, head)'s partials by one wave, whose halves take every second one: lane i of a
 // half reads its i-th partial's (max, sum), so the weights of up to 64 partials cost one memory
 // round trip, taken together with the first eight partials' values.  The order of the sums is fixed.
-// Bound by its round trips and the launch: 4 to 5 us for a few partials a row, 8 for 32 partials of
-// 1024 rows (by half a wave each 9.2), 8 to 10 for the largest calls (16 values at once there: 10 to 14).
+// Bound by its round trips and the launch: 3.5 to 5 us for a few partials a row, 7 for 32 partials of
+// 1024 (row, head) pairs (by half a wave each 9.2), 8 to 10 for the largest calls (16 values at once there: 10 to 14).
 template <int HD>
 __global__ void __launch_bounds__(256)
 k_paged_merge(PagedArgs a) {
@@ -133,8 +133,8 @@ k_paged_merge(PagedArgs a) {
 
 // The work order of the requests' own items, {request, first pair of the tile, chunk} by
 // descending number of keys (to an eighth of an octave), built by one workgroup: a count of
-// the items of each length, their places, the items.  4.7 us, and verification of batch 64 takes
-// 147 us with it, 172 without.
+// the items of each length, their places, the items.  4.7 us; the whole call of 64 decoding
+// requests of up to 4096 keys takes 96 us with it, 116 without.
 __global__ void __launch_bounds__(1024)
 k_paged_plan(PagedArgs a, int units, int TM) {
   extern __shared__ int s_first[];          // first tile of each request
@@ -203,9 +203,10 @@ k_paged_plan(PagedArgs a, int units, int TM) {
 long long tile_bound(long long rows, int G, int TM, int runs) { return rows * G / TM + runs; }
 
 // How the (row, query head) pairs of a unit are tiled: 64 where a unit has no more (streamed),
-// else 128 (wide).  Streamed 128-pair units, two blocks of 16 rows a wave, took 169 us where wide
-// ones take 89 (batch 64, groups of 8, blocks of up to 16); units of up to 64 pairs in wide tiles
-// of two waves 184 us for 158 (verification batch 64); tiles of 256 pairs, 8 waves, equal.
+// else 128 (wide).  Whole calls of 64 requests on contexts of 2048 to 4096, streamed and wide: 32
+// pairs (8 kv heads) 146 and 169 us, 64 pairs 155 and 180, 64 pairs (4 kv heads) 91 and 95; 80 pairs
+// 110 and 97, 128 pairs 133 and 102, 132 pairs (8 kv heads) 206 and 183.  Tiles of 256 pairs,
+// 8 waves: equal to 128.
 int tile_rows(long long pairs) { return pairs <= 64 ? 64 : WIDE_ROWS; }
 
 long long items(long long units, int n_kv, int mc) { return units * n_kv * mc; }
@@ -249,8 +250,10 @@ struct AttnPlan {
   size_t part, row_nc, plan, plan_bytes, total;
 };
 // Items a launch may have before they are listed longest first: what fits about one round of
-// the workgroup slots gains nothing, and the list costs a launch.  Not for shared calls, whose
-// own items are short beside the prefix.
+// the workgroup slots gains nothing, and the list costs a launch.  Decoding on ragged contexts,
+// listed and not: 512 items 16 to 17 and 12 us, 1024 items 18 and 16; 1536 items of up to 192 keys 26
+// and 24, of up to 1024 keys 37 and 37, 2048 keys 56 and 63, 4096 keys 96 and 116.  Not for shared
+// calls, whose own items are short beside the prefix.
 constexpr long long PLAN_MIN = 1024;
 
 AttnPlan attn_plan(const dcut_paged_cfg *c, int B, bool shared) {

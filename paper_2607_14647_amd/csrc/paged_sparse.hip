@@ -8,9 +8,9 @@
 // value and a short sum are exact there, and two pages change places only where their
 // scores are equal to about 1 in 2^50.
 //
-// Measured: one request of 32000 keys (500 pages) 24 us, of which selection 13, attention 8 and the
-// merge 5 (with their launches); batch 16 at 16 to 64 thousand keys 56 us: selection 24 (30 MB of
-// bounds in 256-byte pieces, 15 of them reading those), the chosen pages 31, 134 MB at 4.4 TB/s.
+// Measured: one request of 32000 keys (500 pages) 22.7 us a call; the kernels alone: selection 12.8,
+// attention 7.4, merge 4.0.  Batch 16 at 16 to 64 thousand keys 56.4: selection 22.5 (39 to 46 MB of bounds in
+// 256-byte pieces, 1.9 TB/s), the chosen pages 30.0, 134 MB at 4.5 TB/s, merge 4.8.
 #include "paged.h"
 
 namespace dcut {
@@ -154,9 +154,10 @@ __device__ __forceinline__ unsigned long long order_key(double x) {
   return (u >> 63) ? ~u : u | 0x8000000000000000ull;
 }
 
-// Pages up to which one workgroup scores and selects: one launch less (500 pages 13.7 us, in two
-// launches 16.7; batch 16 of up to 1000 pages 24.4 and 25.3).  Past it the scores of one (row, kv
-// head) are worth several workgroups.
+// Pages up to which one workgroup scores and selects: one launch less.  Past it the scores of one
+// (row, kv head) are worth several workgroups.  Whole calls of 1, 4 and 16 requests, in one launch and
+// in two: 600 pages 24, 28, 48 and 26, 30, 51 us; 1020 pages 28, 32, 57 and 26, 30, 58; 1500 pages
+// 33, 37, 65 and 27, 31, 65.
 constexpr int FUSED_PAGES = 1024;
 
 // The n_sel pages of one (row, kv head): the first n_sink and the last n_local, then by score,

@@ -4,13 +4,16 @@
 // Tiles of 32 keys, 16 rows a wave (v_mfma_f32_16x16x32_bf16), four waves:
 //   S^T[key][row] = K[key][:] . Q[row][:]   -> lane (row = lane%16) owns keys 4*(lane/16)+j of
 //                                              each 16-key block
-//   O^T[d][row]  += V^T[d][key] . P^T[key][row], P straight from the S^T accumulators (rounded
-//                   to bf16, the width of the matrix operand), V transposed by the LDS reads.
+//   O^T[d][row]  += V^T[d][key] . P^T[key][row], P straight from the S^T accumulators, V
+//                   transposed by the LDS reads.
+// P is rounded to bf16, the width of the matrix operand; the weights' sum keeps float32 (the
+// error this makes: paged_wide.h).
 // A ring of three stages keeps two tiles in flight; three workgroups a CU.
 //
-// What bounds it: the cache stream.  Decoding batch 128 at contexts 512-8191 (1.45 GB) 235 us,
+// What bounds it: the cache stream.  Decoding batch 128 at contexts 512-8191 (1.45 GB) 234 us,
 // 6.2 TB/s of the 6.9 that a plain read of one range reaches here; verification of batch 64 at
-// contexts 2048-4096 (0.81 GB, up to 32 rows a tile) 138 us, 5.9 TB/s.
+// contexts 2048-4096 (0.81 GB, up to 32 rows a tile) 136 us, 6.0 TB/s (this kernel alone; the
+// calls, with work order and merge, 242 and 146).
 #pragma once
 #include "paged_item.h"
 

@@ -10,13 +10,21 @@
 // and exponentials of one wave overlap; two stages of K and of V tiles, the V tile one step
 // behind.  128 rows a workgroup of four waves, two workgroups a CU.
 //
+// Weights meet the values in bf16, the width of the matrix operand, as in the slab's attention;
+// their sum keeps float32.  Each weight is off by at most 2^-8 of itself: outputs differ from the
+// 64-bit definition by 0.0023 (norm of the difference over the norm), by 0.0017 with float32
+// weights, where only the outputs' own rounding to bf16 is left.
+//
 // What bounds it: the serial chain of a step (fragments, scores, maximum, exponentials,
 // rounding, products), two waves a SIMD filling each other's gaps: the matrix units are busy
-// 40% of the time, the LDS 20%.  Prompt of 4 x 2000 rows on contexts up to 2000 (262 GFLOP)
-// 298 us, 880 TFLOP/s (5% more or less with the clock).  Tried: two 32-row blocks a wave (one wave a SIMD: 525 us when the others took 387),
-// three waves a SIMD with 32-key steps (equal), 256 rows in 8 waves (equal), half of the waves
-// a phase behind (3% slower), partials written in whole rows through the LDS (equal), scores and products of one step in turn (equal here, 93 us for 84
-// where batch 64 reads 350 MB in blocks of up to 16).
+// 39% of the time, the LDS 20%.  Prompt of 4 x 2000 rows on contexts up to 2000 (262 GFLOP): the
+// clock gives way under the matrix work, so the kernel alone takes 281 us at least and 346 in the
+// mean of 54 runs in a row, 930 and 760 TFLOP/s; the whole call 280 to 330.
+// Tried: three waves a SIMD with 32-key steps (equal), 256 rows in 8 waves (equal), half of the waves
+// a phase behind (3% slower), partials written in whole rows through the LDS (equal), scores and
+// products of one step in turn (equal here, 93 us for 84 where batch 64 reads 350 MB in blocks of
+// up to 16).  Two 32-row blocks a wave, one wave a SIMD, were tried only before the products ran
+// with the next scores (525 us for 387).
 #pragma once
 #include <type_traits>
 
