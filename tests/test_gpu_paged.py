@@ -1076,3 +1076,20 @@ def test_a_run_of_requests(call, shape):
     b.check(out, ls, ref, rows=np.arange(int(b.d[0]), b.M), what=call)
     n = int(b.d[0])
     assert (out[:n] == 7.0).all() and (ls[:n] == 7.0).all() and int(b.err.item()) == 0
+
+
+def test_host_tensors_are_refused():
+    """A tensor on the host beside a cache on the GPU: refused by name, nothing is launched."""
+    need_gpu()
+    b = Batch(seed=48, **ATTN["verify"])
+    b.bounds()
+    out, ls = b.outputs()
+    ws = L.workspace(L.paged_workspace_bytes("attn", b.cfg(), b.B))
+    good = dict(q=b.dq, cu=b.dcu, ctx_len=b.dctx, out=out, ws=ws, lse=ls, dev_err=b.err)
+    for name in good:
+        t = {**good, name: good[name].cpu()}
+        with pytest.raises(L.DcutError, match=f"dcut_paged_attn, {name}:"):
+            L.paged_attn(b.cfg(), b.pages(), b.B, t["q"], t["cu"], t["ctx_len"], t["out"], t["ws"], lse=t["lse"], dev_err=t["dev_err"])
+    with pytest.raises(L.DcutError, match="pages_desc, device"):
+        L.pages_desc(b.dk, b.dv, b.dtable.cpu())
+    assert (out == 7.0).all() and int(b.err.item()) == 0
